@@ -281,8 +281,146 @@ int lora_topk_workspace_size(int64_t V, int64_t d, int64_t k, size_t* bytes);
 int lora_topk_table(const lora_bf16* E, int64_t V, int64_t d, int64_t k, int32_t* table, void* workspace,
                     size_t workspace_bytes, void* stream);
 
+/* ---- Few tokens: sampling from the adapted model ------------------------
+ * Forward of n_proj (1..64) independent adapted projections with 4-bit base
+ * weights for 1 to 16 tokens each, e.g. the q, k and v projections of a layer
+ * while an answer is sampled token by token:
+ *     y = x W^T + (scale x A^T) B^T,   W[n, k] = bf16(s q + b) as lora_q4_weight
+ * The weights are those the training calls use, element for element.  Sums are
+ * held in fp32; scale x A^T is not rounded to bf16 here (lora_linear_fwd_q4
+ * does, since its backward reads it), and y is rounded once.
+ * Fields read: shape, x, A, B, y, Wq (the others are ignored, but W must be
+ * NULL).  Beyond the shapes of the other calls: T is 1 .. 16 and may differ
+ * between projections, d_in is a multiple of 64, d_out any number from 1 on
+ * (rows of y and B are dense: an odd d_out or rank leaves them unaligned).
+ * The paper has no counterpart: its fine-tuning data is given, not sampled. */
+int lora_decode_workspace_size(const lora_proj* projs, int n_proj, size_t* bytes);
+int lora_decode_q4(const lora_proj* projs, int n_proj, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Policy and preference losses ---------------------------------------
+ * Both take the tokens' negative log-probabilities under the model, nll_t =
+ * -log p_t (the token_loss of lora_ce_fwd_bwd), and hand back the loss, its
+ * derivative by each of them, and the gradient of the hidden states: with the
+ * rows d nll_t / d h_t that lora_ce_fwd_bwd writes into its dh,
+ *     dh_t = (d loss / d nll_t) * dh_nll_t,
+ * rounded to bf16 once; rows of derivative zero are zero, whatever dh_nll
+ * holds there (it is not read).  T tokens lie flat, sequence by sequence:
+ * sequence i is [offsets[i], offsets[i+1]); offsets ascend from 0 to T
+ * (checked on the device: lora_read_status then reports LORA_EINVAL and the
+ * outputs are unspecified); a sequence may be empty.  Tokens with mask 0 take no
+ * part: nothing of them is read but the mask, and their derivative is zero.
+ * The sums over tokens are held in fp64, in a fixed order.
+ * Arrays of one value per token, sequence or pair need the alignment of their
+ * type only; dh_nll and dh 16 bytes, and d a multiple of 8.  dh may be dh_nll
+ * (scaled in place); dh NULL: no gradient of the hidden states.
+ * 1 <= T <= 2^24, 1 <= S <= 2^24 (1 <= P <= 2^23). */
+
+/* What the tokens' terms are summed to. */
+enum {
+  LORA_SUM = 0,         /* their sum */
+  LORA_MEAN_TOKENS = 1, /* the mean over the trainable tokens of the batch */
+  LORA_MEAN_SEQS = 2    /* the mean over the S sequences of each one's mean (0 for one without trainable tokens) */
+};
+
+/* Clipped policy loss with a penalty for leaving a reference model.  With the
+ * sampling model's old_nll, the reference model's ref_nll and the advantage A
+ * of the token's sequence (or of the token):
+ *     delta = old_nll - nll,  rho = exp(delta),  e = nll - ref_nll
+ *     l = -min(A rho, A clamp(rho, 1 - clip_low, 1 + clip_high)) + beta (exp(e) - 1 - e)
+ *     loss = scale * (sum, mean or mean of means of l)
+ * A token is clipped (its first term then has no derivative) when A > 0 and
+ * delta > log(1 + clip_high), or A < 0 and delta < log(1 - clip_low), the fp32
+ * difference against the fp32 logarithm.  exp(e) - 1 - e >= 0 estimates the
+ * divergence of the model from the reference on a sampled token; ref_nll NULL:
+ * no such term.  stats[0] receives its mean over the trainable tokens, stats[1]
+ * the share of them that is clipped (0 without any).
+ * 0 <= clip_low <= 1, 0 <= clip_high; clip_high, beta and scale finite. */
+typedef struct lora_policy_args {
+  int64_t T, S, d;
+  const int32_t* offsets;   /* [S + 1] */
+  const float* nll;         /* [T] */
+  const float* old_nll;     /* [T] */
+  const float* ref_nll;     /* [T] or NULL */
+  const float* advantage;   /* [S], or [T] with advantage_per_token */
+  const uint8_t* mask;      /* [T], nonzero = trainable; NULL = every token */
+  const lora_bf16* dh_nll;  /* [T, d]; may be NULL with dh */
+  int advantage_per_token;
+  int reduction;            /* LORA_SUM, LORA_MEAN_TOKENS or LORA_MEAN_SEQS */
+  float clip_low, clip_high, beta, scale;
+  float* loss;              /* [1] */
+  float* stats;             /* [2] or NULL */
+  float* token_weight;      /* [T] or NULL: d loss / d nll_t */
+  lora_bf16* dh;            /* [T, d] or NULL */
+} lora_policy_args;
+
+int lora_policy_workspace_size(const lora_policy_args* args, size_t* bytes);
+int lora_policy_fwd_bwd(const lora_policy_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Loss of P pairs of a preferred and a rejected answer: sequences 2p and
+ * 2p + 1.  With R the sum over a sequence's trainable tokens of ref_nll - nll
+ * (its log-probability ratio to the reference model; ref_nll NULL: its
+ * log-probability), or with mean_tokens their mean (0 without any),
+ *     m = beta (R_2p - R_2p+1) - margin
+ *     LORA_PREF_SIGMOID  l = (1 - label_smoothing) log(1 + exp(-m)) + label_smoothing log(1 + exp(m))
+ *     LORA_PREF_HINGE    l = max(0, 1 - m)
+ *     LORA_PREF_SQUARE   l = ((m - 1/2) / beta)^2
+ *     loss = scale / P * sum l
+ * rewards[i] receives beta R_i.  beta > 0, 0 <= label_smoothing <= 1; beta,
+ * margin and scale finite; label_smoothing is read by LORA_PREF_SIGMOID only. */
+enum { LORA_PREF_SIGMOID = 0, LORA_PREF_HINGE = 1, LORA_PREF_SQUARE = 2 };
+
+typedef struct lora_pref_args {
+  int64_t T, P, d;
+  const int32_t* offsets;   /* [2 P + 1] */
+  const float* nll;         /* [T] */
+  const float* ref_nll;     /* [T] or NULL */
+  const uint8_t* mask;      /* [T] or NULL */
+  const lora_bf16* dh_nll;  /* [T, d]; may be NULL with dh */
+  int kind;
+  int mean_tokens;
+  float beta, margin, label_smoothing, scale;
+  float* loss;              /* [1] */
+  float* rewards;           /* [2 P] or NULL */
+  float* token_weight;      /* [T] or NULL: d loss / d nll_t */
+  lora_bf16* dh;            /* [T, d] or NULL */
+} lora_pref_args;
+
+int lora_pref_workspace_size(const lora_pref_args* args, size_t* bytes);
+int lora_pref_fwd_bwd(const lora_pref_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Gradient clipping ---------------------------------------------------
+ * Global norm of n_grads (1..65536) gradient tensors, such as dA and dB of
+ * every projection, and their clipping:
+ *     norm = sqrt(sum over tensors and elements of src^2)
+ *     coef = norm > max_norm ? max_norm / norm : 1,    dst = coef * src
+ * over dense tensors of n elements, fp32 or bf16, aligned to their type.  dst
+ * is a tensor of the same type: src itself (clipped in place; nothing is
+ * written when coef is 1), one that overlaps no tensor of the call, or NULL
+ * (the tensor counts toward the norm and is not written).  Squares are summed
+ * in fp32 over a few dozen elements and in fp64 from there on (in fp64
+ * throughout where fp32 would overflow or lose small values), in an order that
+ * depends on the tensors' sizes only.  norm (device, [1])
+ * and coef (device, [1], or NULL) are written.  A norm that is not finite (a
+ * gradient holds an infinity or a NaN) makes coef 1: the gradients are passed
+ * on as they are, and the caller sees the norm.  max_norm >= 0, infinity for
+ * the norm alone.  n = 0 is allowed (src and dst may be NULL then).
+ * The table of tensors is read during the call. */
+enum { LORA_F32 = 0, LORA_BF16 = 1 };
+
+typedef struct lora_grad {
+  const void* src;
+  void* dst;
+  int64_t n;
+  int dtype; /* LORA_F32 or LORA_BF16 */
+} lora_grad;
+
+int lora_clip_workspace_size(const lora_grad* grads, int n_grads, size_t* bytes);
+int lora_clip_grads(const lora_grad* grads, int n_grads, float max_norm, float* norm, float* coef, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
 /* Waits for `stream`, then reads the device status word that bounded waits
- * set when they expire (and lora_topk_table sets on an unresolved row):
+ * set when they expire (and lora_topk_table sets on an unresolved row, and the
+ * policy and preference losses on offsets that do not ascend from 0 to T):
  * *status = LORA_OK, LORA_ETIMEOUT or LORA_EINVAL.  reset != 0 clears it.
  * Returns LORA_OK or LORA_ECUDA. */
 int lora_read_status(void* stream, int* status, int reset);

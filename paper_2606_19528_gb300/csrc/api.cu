@@ -2097,6 +2097,132 @@ int topk_check(const lora_bf16* E, int64_t V, int64_t d, int64_t k, TopkPlan* pl
   return LORA_OK;
 }
 
+// ------------------------------------------------------------------ few tokens, policy and preference losses, clipping
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+int decode_check(const lora_proj* projs, int n, size_t* bytes) {
+  if (!projs) return LORA_ENULL;
+  if (n < 1 || n > kDecodeMaxProjs) return LORA_EINVAL;
+  size_t total = 0;
+  for (int i = 0; i < n; ++i) {
+    const lora_shape& s = projs[i].shape;
+    if (s.T < 1 || s.T > kDecodeMaxT || s.d_in < 64 || s.d_in % 64 || s.d_in > (1ll << 20) || s.d_out < 1 ||
+        s.d_out > (1ll << 20) || s.rank < 0 || s.rank > 128 || !isfinite(s.scale))
+      return LORA_EINVAL;
+    total += up256((size_t)s.T * s.rank * sizeof(float));
+  }
+  *bytes = total;
+  return LORA_OK;
+}
+
+int decode_check_ptrs(const lora_proj& p) {
+  if (p.W) return LORA_EINVAL;
+  if (!p.x || !p.y || !p.Wq.codes || !p.Wq.params) return LORA_ENULL;
+  if (p.shape.rank > 0 && (!p.A || !p.B)) return LORA_ENULL;
+  const void* ps[] = {p.x, p.y, p.Wq.codes, p.Wq.params, p.A, p.B};
+  for (const void* q : ps)
+    if (!aligned16(q)) return LORA_EALIGN;
+  return LORA_OK;
+}
+
+struct ObjectivePlan {
+  size_t seq = 0, u = 0, total = 0;
+};
+
+int objective_plan(int64_t T, int64_t groups, int64_t d, ObjectivePlan* pl) {
+  if (T < 1 || T > (1ll << 24) || groups < 1 || groups > (1ll << 24) || d < 8 || d % 8 || d > (1ll << 20))
+    return LORA_EINVAL;
+  pl->u = up256((size_t)groups * sizeof(ObjectiveSeq));
+  pl->total = pl->u + up256((size_t)T * sizeof(float));
+  return LORA_OK;
+}
+
+int policy_check(const lora_policy_args* a, ObjectivePlan* pl) {
+  if (!a) return LORA_ENULL;
+  int rc = objective_plan(a->T, a->S, a->d, pl);
+  if (rc != LORA_OK) return rc;
+  if (a->reduction < LORA_SUM || a->reduction > LORA_MEAN_SEQS) return LORA_EINVAL;
+  if (!(a->clip_low >= 0.f && a->clip_low <= 1.f && a->clip_high >= 0.f) || !isfinite(a->clip_high) ||
+      !isfinite(a->beta) || !isfinite(a->scale))
+    return LORA_EINVAL;
+  if (!a->offsets || !a->nll || !a->old_nll || !a->advantage || !a->loss || (a->dh && !a->dh_nll)) return LORA_ENULL;
+  const void* ps[] = {a->offsets, a->nll, a->old_nll, a->ref_nll, a->advantage, a->loss, a->stats, a->token_weight};
+  for (const void* q : ps)
+    if (!aligned4(q)) return LORA_EALIGN;
+  return aligned16(a->dh_nll) && aligned16(a->dh) ? LORA_OK : LORA_EALIGN;
+}
+
+int pref_check(const lora_pref_args* a, ObjectivePlan* pl) {
+  if (!a) return LORA_ENULL;
+  if (a->P > (1ll << 23)) return LORA_EINVAL;
+  int rc = objective_plan(a->T, a->P, a->d, pl);
+  if (rc != LORA_OK) return rc;
+  if (a->kind < LORA_PREF_SIGMOID || a->kind > LORA_PREF_SQUARE) return LORA_EINVAL;
+  if (!(a->beta > 0.f) || !isfinite(a->beta) || !isfinite(a->margin) || !isfinite(a->scale)) return LORA_EINVAL;
+  if (a->kind == LORA_PREF_SIGMOID && !(a->label_smoothing >= 0.f && a->label_smoothing <= 1.f)) return LORA_EINVAL;
+  if (!a->offsets || !a->nll || !a->loss || (a->dh && !a->dh_nll)) return LORA_ENULL;
+  const void* ps[] = {a->offsets, a->nll, a->ref_nll, a->loss, a->rewards, a->token_weight};
+  for (const void* q : ps)
+    if (!aligned4(q)) return LORA_EALIGN;
+  return aligned16(a->dh_nll) && aligned16(a->dh) ? LORA_OK : LORA_EALIGN;
+}
+
+// Runs `launch(batch, first partial sum, CTAs)` over the tensors in batches that fit a launch's table (the tensors
+// without elements left out); *partials: the batches' partial sums together.  Planned for kPlanSms SMs.
+template <typename Launch>
+int clip_batches(const lora_grad* grads, int n, int* partials, Launch launch) {
+  ClipBatch b;
+  b.n = b.chunks = 0;
+  *partials = 0;
+  auto flush = [&]() -> int {
+    if (!b.n) return LORA_OK;
+    const int ctas = clip_ctas(b.chunks, kPlanSms);
+    const int rc = launch(b, *partials, ctas);
+    *partials += ctas;
+    b.n = b.chunks = 0;
+    return rc;
+  };
+  int rc;
+  for (int i = 0; i < n; ++i) {
+    const lora_grad& g = grads[i];
+    if (!g.n) continue;
+    const int chunks = cdiv(g.n, kClipChunk);  // at most 2^25
+    if ((b.n == kClipTensors || b.chunks > (1 << 30)) && (rc = flush()) != LORA_OK) return rc;
+    ClipTensor& t = b.t[b.n++];
+    t.src = g.src;
+    t.dst = g.dst;
+    t.n = g.n;
+    t.chunk_begin = b.chunks;
+    t.half = g.dtype == LORA_BF16;
+    b.chunks += chunks;
+  }
+  return flush();
+}
+
+int clip_check(const lora_grad* grads, int n, size_t* bytes) {
+  if (!grads) return LORA_ENULL;
+  if (n < 1 || n > 65536) return LORA_EINVAL;
+  for (int i = 0; i < n; ++i) {
+    const lora_grad& g = grads[i];
+    if (g.n < 0 || g.n > (1ll << 38) || (g.dtype != LORA_F32 && g.dtype != LORA_BF16)) return LORA_EINVAL;
+  }
+  int partials = 0;
+  clip_batches(grads, n, &partials, [](const ClipBatch&, int, int) { return LORA_OK; });
+  *bytes = up256((size_t)partials * sizeof(double)) + 256;
+  return LORA_OK;
+}
+
+int clip_check_ptrs(const lora_grad* grads, int n) {
+  for (int i = 0; i < n; ++i) {
+    const lora_grad& g = grads[i];
+    if (!g.n) continue;
+    if (!g.src) return LORA_ENULL;
+    const uintptr_t low = g.dtype == LORA_BF16 ? 1 : 3;
+    if ((reinterpret_cast<uintptr_t>(g.src) | reinterpret_cast<uintptr_t>(g.dst)) & low) return LORA_EALIGN;
+  }
+  return LORA_OK;
+}
+
 }  // namespace
 
 void note_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
@@ -2551,6 +2677,168 @@ int lora_topk_table(const lora_bf16* E, int64_t V, int64_t d, int64_t k, int32_t
   return rec(LORA_OK);
 }
 
+int lora_decode_workspace_size(const lora_proj* projs, int n_proj, size_t* bytes) {
+  if (!bytes) return rec(LORA_ENULL);
+  return rec(decode_check(projs, n_proj, bytes));
+}
+
+int lora_decode_q4(const lora_proj* projs, int n_proj, void* workspace, size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  int rc = decode_check(projs, n_proj, &need);
+  if (rc != LORA_OK) return rec(rc);
+  for (int i = 0; i < n_proj; ++i)
+    if ((rc = decode_check_ptrs(projs[i])) != LORA_OK) return rec(rc);
+  if (need && (rc = check_ws(workspace, workspace_bytes, need)) != LORA_OK) return rec(rc);
+  DeviceInfo* d = nullptr;
+  if ((rc = device_info(&d)) != LORA_OK) return rec(rc);
+  DecodeBatch b;
+  b.n = n_proj;
+  size_t off = 0;
+  for (int i = 0; i < n_proj; ++i) {
+    const lora_proj& q = projs[i];
+    DecodeProj& p = b.p[i];
+    p.codes = q.Wq.codes;
+    p.params = cb(q.Wq.params);
+    p.x = cb(q.x);
+    p.A = cb(q.A);
+    p.B = cb(q.B);
+    p.y = mb(q.y);
+    p.su = at<float>(workspace, off);
+    p.scale = q.shape.scale;
+    p.T = (int)q.shape.T;
+    p.N = (int)q.shape.d_out;
+    p.K = (int)q.shape.d_in;
+    p.r = (int)q.shape.rank;
+    off += up256((size_t)p.T * p.r * sizeof(float));
+  }
+  return rec(launch_decode(b, d->num_sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LORA_OK : LORA_ECUDA);
+}
+
+int lora_policy_workspace_size(const lora_policy_args* args, size_t* bytes) {
+  if (!bytes) return rec(LORA_ENULL);
+  ObjectivePlan pl;
+  const int rc = policy_check(args, &pl);
+  if (rc != LORA_OK) return rec(rc);
+  *bytes = pl.total;
+  return rec(LORA_OK);
+}
+
+int lora_policy_fwd_bwd(const lora_policy_args* a, void* workspace, size_t workspace_bytes, void* stream) {
+  ObjectivePlan pl;
+  int rc = policy_check(a, &pl);
+  if (rc != LORA_OK) return rec(rc);
+  if ((rc = check_ws(workspace, workspace_bytes, pl.total)) != LORA_OK) return rec(rc);
+  DeviceInfo* d = nullptr;
+  if ((rc = device_info(&d)) != LORA_OK) return rec(rc);
+  Objective o;
+  memset(&o, 0, sizeof(o));
+  o.offsets = a->offsets;
+  o.nll = a->nll;
+  o.old_nll = a->old_nll;
+  o.ref_nll = a->ref_nll;
+  o.adv = a->advantage;
+  o.mask = a->mask;
+  o.T = (int)a->T;
+  o.groups = (int)a->S;
+  o.d = (int)a->d;
+  o.per_token = a->advantage_per_token != 0;
+  o.reduction = a->reduction;
+  o.clip_low = a->clip_low;
+  o.clip_high = a->clip_high;
+  o.log_low = (float)log1p(-(double)a->clip_low);  // -infinity for clip_low 1: never below it
+  o.log_high = (float)log1p((double)a->clip_high);
+  o.beta = a->beta;
+  o.scale = a->scale;
+  o.dh_nll = cb(a->dh_nll);
+  o.loss = a->loss;
+  o.stats = a->stats;
+  o.token_weight = a->token_weight;
+  o.dh = mb(a->dh);
+  o.seq = at<ObjectiveSeq>(workspace, pl.seq);
+  o.u = at<float>(workspace, pl.u);
+  o.status = d->status;
+  return rec(launch_policy(o, d->num_sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LORA_OK : LORA_ECUDA);
+}
+
+int lora_pref_workspace_size(const lora_pref_args* args, size_t* bytes) {
+  if (!bytes) return rec(LORA_ENULL);
+  ObjectivePlan pl;
+  const int rc = pref_check(args, &pl);
+  if (rc != LORA_OK) return rec(rc);
+  *bytes = pl.total;
+  return rec(LORA_OK);
+}
+
+int lora_pref_fwd_bwd(const lora_pref_args* a, void* workspace, size_t workspace_bytes, void* stream) {
+  ObjectivePlan pl;
+  int rc = pref_check(a, &pl);
+  if (rc != LORA_OK) return rec(rc);
+  if ((rc = check_ws(workspace, workspace_bytes, pl.total)) != LORA_OK) return rec(rc);
+  DeviceInfo* d = nullptr;
+  if ((rc = device_info(&d)) != LORA_OK) return rec(rc);
+  Objective o;
+  memset(&o, 0, sizeof(o));
+  o.offsets = a->offsets;
+  o.nll = a->nll;
+  o.ref_nll = a->ref_nll;
+  o.mask = a->mask;
+  o.T = (int)a->T;
+  o.groups = (int)a->P;
+  o.d = (int)a->d;
+  o.reduction = LORA_SUM;  // the weights hold the whole factor
+  o.beta = a->beta;
+  o.scale = a->scale;
+  o.kind = a->kind;
+  o.mean_tokens = a->mean_tokens != 0;
+  o.margin = a->margin;
+  o.smoothing = a->label_smoothing;
+  o.dh_nll = cb(a->dh_nll);
+  o.loss = a->loss;
+  o.rewards = a->rewards;
+  o.token_weight = a->token_weight;
+  o.dh = mb(a->dh);
+  o.seq = at<ObjectiveSeq>(workspace, pl.seq);
+  o.u = at<float>(workspace, pl.u);
+  o.status = d->status;
+  return rec(launch_pref(o, d->num_sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LORA_OK : LORA_ECUDA);
+}
+
+int lora_clip_workspace_size(const lora_grad* grads, int n_grads, size_t* bytes) {
+  if (!bytes) return rec(LORA_ENULL);
+  return rec(clip_check(grads, n_grads, bytes));
+}
+
+int lora_clip_grads(const lora_grad* grads, int n_grads, float max_norm, float* norm, float* coef, void* workspace,
+                    size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  int rc = clip_check(grads, n_grads, &need);
+  if (rc != LORA_OK) return rec(rc);
+  if (!(max_norm >= 0.f)) return rec(LORA_EINVAL);
+  if (!norm) return rec(LORA_ENULL);
+  if ((rc = clip_check_ptrs(grads, n_grads)) != LORA_OK) return rec(rc);
+  if (!aligned4(norm) || !aligned4(coef)) return rec(LORA_EALIGN);
+  if ((rc = check_ws(workspace, workspace_bytes, need)) != LORA_OK) return rec(rc);
+  DeviceInfo* d = nullptr;
+  if ((rc = device_info(&d)) != LORA_OK) return rec(rc);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  double* partial = at<double>(workspace, 0);
+  int partials = 0, again = 0;
+  rc = clip_batches(grads, n_grads, &partials, [&](const ClipBatch& b, int first, int ctas) {
+    return launch_clip_sum(b, partial + first, ctas, st) == cudaSuccess ? LORA_OK : LORA_ECUDA;
+  });
+  if (rc != LORA_OK) return rec(rc);
+  auto scale = [&](const ClipBatch& b, int, int ctas) {
+    return launch_clip_scale(b, partial, partials, max_norm, norm, coef, ctas, st) == cudaSuccess ? LORA_OK
+                                                                                                  : LORA_ECUDA;
+  };
+  if (partials == 0) {  // no element: norm 0
+    ClipBatch b;
+    b.n = b.chunks = 0;
+    return rec(scale(b, 0, 1));
+  }
+  return rec(clip_batches(grads, n_grads, &again, scale));
+}
+
 int lora_wait_selftest(int64_t limit_ns, void* stream) {
   if (limit_ns < 1000 || limit_ns > 1000000000ll) return rec(LORA_EINVAL);
   DeviceInfo* d = nullptr;
@@ -2569,7 +2857,7 @@ int lora_read_status(void* stream, int* status, int reset) {
     const int z = 0;
     if (cudaMemcpyToSymbol(g_status, &z, sizeof(int)) != cudaSuccess) return rec(LORA_ECUDA);
   }
-  *status = v == 0 ? LORA_OK : v == kStatusTopkTies ? LORA_EINVAL : LORA_ETIMEOUT;
+  *status = v == 0 ? LORA_OK : v == kStatusTopkTies || v == kStatusOffsets ? LORA_EINVAL : LORA_ETIMEOUT;
   return rec(LORA_OK);
 }
 

@@ -17,6 +17,7 @@ namespace lora {
 // Error codes written to the device status word (first error wins).
 constexpr int kStatusTimeout = 1;
 constexpr int kStatusTopkTies = 2;  // a top-k row had more candidates tied at its k-th value than fit
+constexpr int kStatusOffsets = 3;   // sequence offsets that do not ascend from 0 to T
 
 struct WaitCtl {
   int* status;         // device status word

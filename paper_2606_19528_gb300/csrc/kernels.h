@@ -392,4 +392,83 @@ cudaError_t launch_wait_probe(int* status, long long limit_ns, cudaStream_t stre
 cudaError_t launch_pad_cols(const __nv_bfloat16* src, int rows, int r, __nv_bfloat16* dst, int ld_dst,
                             cudaStream_t stream);
 
+// ---------------------------------------------------------------- few tokens, 4-bit weights
+constexpr int kDecodeMaxT = 16;      // tokens of one call
+constexpr int kDecodeMaxProjs = 64;  // projections of one call
+
+struct DecodeProj {
+  const uint8_t* codes;         // [N, K / 2]
+  const __nv_bfloat16* params;  // [N, K / 64, 2]: (s, b)
+  const __nv_bfloat16* x;       // [T, K]
+  const __nv_bfloat16* A;       // [r, K]
+  const __nv_bfloat16* B;       // [N, r]
+  __nv_bfloat16* y;             // [T, N]
+  float* su;                    // [T, r]: scale * x A^T, written by the first launch
+  float scale;
+  int T, N, K, r;
+  int tile_begin;  // first of its row tiles in the launch's list
+  int row_begin;   // first of its adapter rows in the first launch's list
+};
+
+struct DecodeBatch {
+  DecodeProj p[kDecodeMaxProjs];
+  int n, tiles, rows;
+};
+
+// su of every projection with an adapter (nothing to launch without one), then y = x W^T + su B^T.  The caller
+// sets all but the begins and the totals.
+cudaError_t launch_decode(DecodeBatch& b, int num_sms, cudaStream_t stream);
+
+// ---------------------------------------------------------------- policy and preference losses
+struct ObjectiveSeq {  // what the first launch leaves per sequence (policy) or pair (preference)
+  double loss, kl;
+  int n, clipped;
+};
+
+struct Objective {
+  // tokens
+  const int32_t* offsets;
+  const float *nll, *old_nll, *ref_nll, *adv;
+  const uint8_t* mask;
+  int T, groups, d;  // groups: sequences (policy) or pairs (preference)
+  // policy
+  int per_token, reduction;
+  float clip_low, clip_high, log_low, log_high, beta, scale;
+  // preference
+  int kind, mean_tokens;
+  float margin, smoothing;
+  // outputs
+  const __nv_bfloat16* dh_nll;
+  float *loss, *stats, *rewards, *token_weight;
+  __nv_bfloat16* dh;
+  // workspace
+  ObjectiveSeq* seq;  // [groups]
+  float* u;           // [T]: the tokens' weights, but for the factor 1 / (trainable tokens)
+  int* status;
+};
+cudaError_t launch_policy(const Objective& o, int num_sms, cudaStream_t stream);
+cudaError_t launch_pref(const Objective& o, int num_sms, cudaStream_t stream);
+
+// ---------------------------------------------------------------- gradient norm and clipping
+struct ClipTensor {
+  const void* src;
+  void* dst;  // null: counted, not written
+  long long n;
+  int chunk_begin;  // first of its chunks in the launch's list
+  int half;         // 1: bf16, 0: fp32
+};
+constexpr int kClipTensors = 1000;  // per launch: the table is a kernel argument, at most 32764 bytes
+constexpr int kClipChunk = 8192;    // elements
+
+struct ClipBatch {
+  ClipTensor t[kClipTensors];
+  int n, chunks;
+};
+// partial[0 .. ctas) = the CTAs' sums of squares over the batch; ctas = clip_ctas(chunks, num_sms).
+int clip_ctas(int chunks, int num_sms);
+cudaError_t launch_clip_sum(const ClipBatch& b, double* partial, int ctas, cudaStream_t stream);
+// dst = src min(1, max_norm / norm) over the batch, norm from partial[0 .. n_partial).
+cudaError_t launch_clip_scale(const ClipBatch& b, const double* partial, int n_partial, float max_norm, float* norm,
+                              float* coef, int ctas, cudaStream_t stream);
+
 }  // namespace lora

@@ -30,11 +30,24 @@ LORA_FWD = 1
 LORA_BWD = 2
 LORA_FWD_BWD = 3
 
+LORA_SUM = 0
+LORA_MEAN_TOKENS = 1
+LORA_MEAN_SEQS = 2
+
+LORA_PREF_SIGMOID = 0
+LORA_PREF_HINGE = 1
+LORA_PREF_SQUARE = 2
+
+LORA_F32 = 0
+LORA_BF16 = 1
+
 # every symbol that include/lora.h declares
 EXPORTS = ("lora_workspace_size", "lora_linear_fwd", "lora_linear_fwd_noalloc", "lora_linear_bwd",
            "lora_linear_fwd_q4", "lora_linear_bwd_q4", "lora_stack_workspace_size",
            "lora_stack_step", "lora_stack_ckpt_workspace_size", "lora_stack_ckpt", "lora_ce_workspace_size",
-           "lora_ce_fwd_bwd", "lora_topk_workspace_size", "lora_topk_table", "lora_wait_selftest",
+           "lora_ce_fwd_bwd", "lora_topk_workspace_size", "lora_topk_table", "lora_decode_workspace_size",
+           "lora_decode_q4", "lora_policy_workspace_size", "lora_policy_fwd_bwd", "lora_pref_workspace_size",
+           "lora_pref_fwd_bwd", "lora_clip_workspace_size", "lora_clip_grads", "lora_wait_selftest",
            "lora_read_status", "lora_set_wait_limit_ns", "lora_launch_count",
            "lora_profile_begin", "lora_profile_begin_kinds", "lora_profile_end", "lora_strerror", "lora_version",
            "lora_last_error")
@@ -79,6 +92,29 @@ class lora_ce_args(ctypes.Structure):
                 ("dh", ctypes.c_void_p), ("vocab", ctypes.c_void_p), ("counts", ctypes.c_void_p)]
 
 
+class lora_policy_args(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("S", ctypes.c_int64), ("d", ctypes.c_int64),
+                ("offsets", ctypes.c_void_p), ("nll", ctypes.c_void_p), ("old_nll", ctypes.c_void_p),
+                ("ref_nll", ctypes.c_void_p), ("advantage", ctypes.c_void_p), ("mask", ctypes.c_void_p),
+                ("dh_nll", ctypes.c_void_p), ("advantage_per_token", ctypes.c_int), ("reduction", ctypes.c_int),
+                ("clip_low", ctypes.c_float), ("clip_high", ctypes.c_float), ("beta", ctypes.c_float),
+                ("scale", ctypes.c_float), ("loss", ctypes.c_void_p), ("stats", ctypes.c_void_p),
+                ("token_weight", ctypes.c_void_p), ("dh", ctypes.c_void_p)]
+
+
+class lora_pref_args(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int64), ("P", ctypes.c_int64), ("d", ctypes.c_int64),
+                ("offsets", ctypes.c_void_p), ("nll", ctypes.c_void_p), ("ref_nll", ctypes.c_void_p),
+                ("mask", ctypes.c_void_p), ("dh_nll", ctypes.c_void_p), ("kind", ctypes.c_int),
+                ("mean_tokens", ctypes.c_int), ("beta", ctypes.c_float), ("margin", ctypes.c_float),
+                ("label_smoothing", ctypes.c_float), ("scale", ctypes.c_float), ("loss", ctypes.c_void_p),
+                ("rewards", ctypes.c_void_p), ("token_weight", ctypes.c_void_p), ("dh", ctypes.c_void_p)]
+
+
+class lora_grad(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int)]
+
+
 def library(path: str = _LIB_PATH) -> ctypes.CDLL:
     """Load the CUDA library (once).  Raises OSError if it has not been built."""
     global _lib
@@ -103,6 +139,14 @@ def library(path: str = _LIB_PATH) -> ctypes.CDLL:
         lib.lora_ce_fwd_bwd.argtypes = [P(lora_ce_args), vp, sz, vp]
         lib.lora_topk_workspace_size.argtypes = [i64, i64, i64, P(sz)]
         lib.lora_topk_table.argtypes = [vp, i64, i64, i64, vp, vp, sz, vp]
+        lib.lora_decode_workspace_size.argtypes = [P(lora_proj), i32, P(sz)]
+        lib.lora_decode_q4.argtypes = [P(lora_proj), i32, vp, sz, vp]
+        lib.lora_policy_workspace_size.argtypes = [P(lora_policy_args), P(sz)]
+        lib.lora_policy_fwd_bwd.argtypes = [P(lora_policy_args), vp, sz, vp]
+        lib.lora_pref_workspace_size.argtypes = [P(lora_pref_args), P(sz)]
+        lib.lora_pref_fwd_bwd.argtypes = [P(lora_pref_args), vp, sz, vp]
+        lib.lora_clip_workspace_size.argtypes = [P(lora_grad), i32, P(sz)]
+        lib.lora_clip_grads.argtypes = [P(lora_grad), i32, ctypes.c_float, vp, vp, vp, sz, vp]
         lib.lora_wait_selftest.argtypes = [i64, vp]
         lib.lora_read_status.argtypes = [vp, P(i32), i32]
         lib.lora_set_wait_limit_ns.argtypes = [i64]
@@ -198,9 +242,13 @@ def lora_linear_bwd_q4(shape, dy, x, Wq: lora_q4_weight, A, B, su, dx, dA, dB, w
                                         int(workspace_bytes), _stream(stream)), "lora_linear_bwd_q4")
 
 
-def _proj_array(projs):
-    arr = (lora_proj * len(projs))(*projs)
-    return arr
+def make_projs(projs):
+    """The C array of a list of projections.  Calls that take projections also take such an array as it is: a
+    program that calls again on the same buffers makes it once."""
+    return projs if isinstance(projs, ctypes.Array) else (lora_proj * len(projs))(*projs)
+
+
+_proj_array = make_projs
 
 
 def lora_stack_workspace_size(projs, mode: int) -> int:
@@ -271,6 +319,91 @@ def lora_topk_table(E, V: int, d: int, k: int, table, workspace, workspace_bytes
     """Top-k cosine-similarity table of the embedding E [V, d] into table [V, k] int32."""
     _check(library().lora_topk_table(_ptr(E), int(V), int(d), int(k), _ptr(table), _ptr(workspace),
                                      int(workspace_bytes), _stream(stream)), "lora_topk_table")
+
+
+def lora_decode_workspace_size(projs) -> int:
+    arr = make_projs(projs)
+    n = ctypes.c_size_t(0)
+    _check(library().lora_decode_workspace_size(arr, len(arr), ctypes.byref(n)), "lora_decode_workspace_size")
+    return n.value
+
+
+def lora_decode_q4(projs, workspace, workspace_bytes, stream=None) -> None:
+    """Forward of adapted projections with 4-bit base weights for 1 to 16 tokens (see include/lora.h).
+    `projs`: a list of projections, or their array from make_projs."""
+    arr = make_projs(projs)
+    _check(library().lora_decode_q4(arr, len(arr), _ptr(workspace), int(workspace_bytes), _stream(stream)),
+           "lora_decode_q4")
+
+
+def make_policy_args(T, S, d, offsets, nll, old_nll, advantage, loss, ref_nll=None, mask=None,
+                     advantage_per_token=False, clip_low=0.2, clip_high=0.2, beta=0.0, scale=1.0,
+                     reduction=LORA_MEAN_TOKENS, dh_nll=None, dh=None, token_weight=None,
+                     stats=None) -> lora_policy_args:
+    return lora_policy_args(int(T), int(S), int(d), _ptr(offsets), _ptr(nll), _ptr(old_nll), _ptr(ref_nll),
+                            _ptr(advantage), _ptr(mask), _ptr(dh_nll), int(bool(advantage_per_token)),
+                            int(reduction), float(clip_low), float(clip_high), float(beta), float(scale),
+                            _ptr(loss), _ptr(stats), _ptr(token_weight), _ptr(dh))
+
+
+def lora_policy_workspace_size(args: lora_policy_args) -> int:
+    n = ctypes.c_size_t(0)
+    _check(library().lora_policy_workspace_size(ctypes.byref(args), ctypes.byref(n)), "lora_policy_workspace_size")
+    return n.value
+
+
+def lora_policy_fwd_bwd(args: lora_policy_args, workspace, workspace_bytes, stream=None) -> None:
+    """Clipped policy loss with a KL term and its gradient (see include/lora.h)."""
+    _check(library().lora_policy_fwd_bwd(ctypes.byref(args), _ptr(workspace), int(workspace_bytes),
+                                         _stream(stream)), "lora_policy_fwd_bwd")
+
+
+def make_pref_args(T, P, d, offsets, nll, loss, ref_nll=None, mask=None, kind=LORA_PREF_SIGMOID, mean_tokens=False,
+                   beta=0.1, margin=0.0, label_smoothing=0.0, scale=1.0, dh_nll=None, dh=None, token_weight=None,
+                   rewards=None) -> lora_pref_args:
+    return lora_pref_args(int(T), int(P), int(d), _ptr(offsets), _ptr(nll), _ptr(ref_nll), _ptr(mask), _ptr(dh_nll),
+                          int(kind), int(bool(mean_tokens)), float(beta), float(margin), float(label_smoothing),
+                          float(scale), _ptr(loss), _ptr(rewards), _ptr(token_weight), _ptr(dh))
+
+
+def lora_pref_workspace_size(args: lora_pref_args) -> int:
+    n = ctypes.c_size_t(0)
+    _check(library().lora_pref_workspace_size(ctypes.byref(args), ctypes.byref(n)), "lora_pref_workspace_size")
+    return n.value
+
+
+def lora_pref_fwd_bwd(args: lora_pref_args, workspace, workspace_bytes, stream=None) -> None:
+    """Loss of pairs of a preferred and a rejected answer and its gradient (see include/lora.h)."""
+    _check(library().lora_pref_fwd_bwd(ctypes.byref(args), _ptr(workspace), int(workspace_bytes), _stream(stream)),
+           "lora_pref_fwd_bwd")
+
+
+def make_grads(pairs):
+    """The C array of gradient tensors from (src, dst) pairs of contiguous fp32 or bf16 tensors of one size and
+    type; dst None: counted in the norm and not written."""
+    import torch
+    dtypes = {torch.float32: LORA_F32, torch.bfloat16: LORA_BF16}
+    arr = (lora_grad * len(pairs))()
+    for g, (src, dst) in zip(arr, pairs):
+        if src.dtype not in dtypes:
+            raise TypeError(f"gradients are float32 or bfloat16, not {src.dtype}")
+        for t in (src, dst):
+            if t is not None and (t.dtype != src.dtype or t.numel() != src.numel() or not t.is_contiguous()):
+                raise ValueError("src and dst are contiguous tensors of one size and type")
+        g.src, g.dst, g.n, g.dtype = src.data_ptr(), _ptr(dst), src.numel(), dtypes[src.dtype]
+    return arr
+
+
+def lora_clip_workspace_size(grads) -> int:
+    n = ctypes.c_size_t(0)
+    _check(library().lora_clip_workspace_size(grads, len(grads), ctypes.byref(n)), "lora_clip_workspace_size")
+    return n.value
+
+
+def lora_clip_grads(grads, max_norm: float, norm, coef, workspace, workspace_bytes, stream=None) -> None:
+    """Global norm of the gradient tensors `grads` (from make_grads) and their clipping (see include/lora.h)."""
+    _check(library().lora_clip_grads(grads, len(grads), float(max_norm), _ptr(norm), _ptr(coef), _ptr(workspace),
+                                     int(workspace_bytes), _stream(stream)), "lora_clip_grads")
 
 
 def lora_wait_selftest(limit_ns: int, stream=None) -> None:

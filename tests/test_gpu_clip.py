@@ -1,0 +1,188 @@
+"""GPU parity of the gradient norm and clipping through the C ABI, against the
+fp64 oracle.
+
+Tolerances: squares of fp32 are summed in fp32 over a few dozen elements and
+in fp64 beyond: 64 roundings of 2^-24 bound the norm's relative error by 2e-6
+(half of it, in fact: the root).  A clipped element is one product with a
+coefficient rounded to fp32: three roundings on top of the norm's error; one
+more of 2^-9 for bf16.  A product below the normal range of either type has its
+spacing there, 2^-149 for fp32 and 2^-133 for bf16."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2606_19528_gb300 import lora
+from tests import gpu_util as G
+
+pytestmark = pytest.mark.gpu
+
+NAN = float("nan")
+
+
+def run(pairs, max_norm, coef=True):
+    arr = lora.make_grads(pairs)
+    norm, cf = torch.full((3,), NAN, device="cuda"), torch.full((3,), NAN, device="cuda")
+    n = lora.lora_clip_workspace_size(arr)
+    ws = torch.full((n + 256,), 0x7f, dtype=torch.uint8, device="cuda")
+    lora.lora_clip_grads(arr, max_norm, norm[1:], cf[1:] if coef else None, ws, n)
+    torch.cuda.synchronize()
+    assert (ws[n:] == 0x7f).all()
+    assert torch.isnan(norm[0]) and torch.isnan(norm[2]) and torch.isnan(cf[0]) and torch.isnan(cf[2])
+    return float(norm[1]), float(cf[1])
+
+
+def tensors(seed, sizes, dtypes=(torch.float32,), std=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return [(std * torch.randn(n, generator=g, device="cuda")).to(dtypes[i % len(dtypes)])
+            for i, n in enumerate(sizes)]
+
+
+def check(grads, outs, max_norm, in_place=False):
+    """outs: same-shaped destinations; in_place: they are the grads."""
+    src = [G.host_f64(g) for g in grads]
+    want_norm, want_coef, want = oracle.clip_grads(src, max_norm)
+    norm, coef = run(list(zip(grads, outs)), max_norm)
+    assert norm == pytest.approx(want_norm, rel=2e-6)
+    assert coef == pytest.approx(want_coef, rel=2e-6)
+    for g, o, w in zip(grads, outs, want):
+        if o is not None:
+            tol, step = (3e-6, 2.0 ** -149) if o.dtype == torch.float32 else (2.0 ** -8, 2.0 ** -133)
+            assert (np.abs(G.host_f64(o) - w) <= tol * np.abs(w) + step).all()
+    return coef
+
+
+SIZES = [[1], [3], [1, 1, 1], [8191, 8192, 8193], [100000], [49152, 16384, 49152, 4096], [5, 70001, 12, 333, 8192 * 3]]
+
+
+@pytest.mark.parametrize("sizes", SIZES)
+@pytest.mark.parametrize("dtypes", [(torch.float32,), (torch.bfloat16,), (torch.float32, torch.bfloat16)])
+@pytest.mark.parametrize("frac", [0.3, 2.0])
+def test_clip(sizes, dtypes, frac):
+    grads = tensors(len(sizes), sizes, dtypes, 0.01)
+    outs = [torch.full_like(g, NAN) for g in grads]
+    limit = frac * 0.01 * math.sqrt(sum(sizes)) + (10.0 if frac > 1 else 0.0)
+    coef = check(grads, outs, limit)
+    if frac > 1:
+        assert coef == 1.0 and all(torch.equal(g, o) for g, o in zip(grads, outs))
+    same = [g.clone() for g in grads]
+    assert check(same, same, limit) == coef
+    assert all(torch.equal(a, b) for a, b in zip(same, outs))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [1, 2, 7, 9, 255, 8190, 8200, 30001])
+def test_unaligned_slices(dtype, n):
+    """Every offset of source and destination from a 16-byte boundary; the neighbours stay."""
+    for a in range(0, 9 if dtype == torch.bfloat16 else 5):
+        for b in {a, 0, 1, 3}:
+            src = tensors(a, [n + 16], (dtype,))[0]
+            dst = torch.full((n + 16,), 9.0, dtype=dtype, device="cuda")
+            check([src[a:a + n]], [dst[b:b + n]], 0.25)
+            assert (dst[:b] == 9).all() and (dst[b + n:] == 9).all()
+            keep = src.clone()
+            check([src[a:a + n]], [src[a:a + n]], 0.25)
+            assert torch.equal(src[:a], keep[:a]) and torch.equal(src[a + n:], keep[a + n:])
+
+
+def test_norm_alone_and_tensors_that_are_only_counted():
+    grads = tensors(1, [1000, 33, 4096])
+    keep = [g.clone() for g in grads]
+    out = torch.full_like(grads[1], NAN)
+    want = math.sqrt(sum(float(g.double().square().sum()) for g in grads))
+    norm, coef = run([(grads[0], None), (grads[1], out), (grads[2], None)], 2.0)
+    assert norm == pytest.approx(want, rel=2e-6) and coef == pytest.approx(2.0 / want, rel=2e-6)
+    assert torch.allclose(out, grads[1] * coef, rtol=1e-6, atol=0)
+    norm, coef = run([(g, g) for g in grads], math.inf)
+    assert norm == pytest.approx(want, rel=2e-6) and coef == 1.0
+    assert all(torch.equal(a, b) for a, b in zip(grads, keep))
+    arr = lora.make_grads([(g, None) for g in grads])
+    only = torch.empty(1, device="cuda")
+    ws = G.workspace(lora.lora_clip_workspace_size(arr))
+    lora.lora_clip_grads(arr, 1.0, only, None, ws, ws.numel())
+    assert float(only) == norm
+
+
+def test_empty_and_zero_tensors():
+    empty = torch.empty(0, device="cuda")
+    assert run([(empty, empty)], 1.0) == (0.0, 1.0)
+    z = torch.zeros(10, device="cuda")
+    assert run([(z, z), (empty, None)], 0.0) == (0.0, 1.0)
+    g = torch.ones(10, device="cuda")
+    norm, coef = run([(empty, empty), (g, g), (empty, None)], 0.0)
+    assert norm == pytest.approx(math.sqrt(10)) and coef == 0.0 and (g == 0).all()
+
+
+@pytest.mark.parametrize("std", [1e-30, 1e-22, 1e-12, 1e12, 1e25, 1e36])
+def test_whole_range_of_fp32(std):
+    """Squares that fp32 cannot hold, alone and beside ordinary values."""
+    grads = tensors(2, [5000, 123], std=std)
+    outs = [torch.empty_like(g) for g in grads]
+    check(grads, outs, 0.5 * std * math.sqrt(5123))
+    mixed = grads + tensors(3, [777])
+    check(mixed, [torch.empty_like(g) for g in mixed], 1e-3)
+
+
+def test_large_values_in_one_place():
+    """One element whose square overflows among small ones of the same thread's."""
+    g = torch.full((30000,), 1e-3, device="cuda")
+    g[12345] = 3e30
+    check([g], [torch.empty_like(g)], 1.0)
+
+
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), NAN])
+def test_not_finite(bad):
+    grads = tensors(4, [9000, 50])
+    grads[0][8500] = bad
+    outs = [torch.zeros_like(g) for g in grads]
+    norm, coef = run(list(zip(grads, outs)), 0.1)
+    assert not math.isfinite(norm) and coef == 1.0
+    assert all(torch.equal(a.view(torch.int32), b.view(torch.int32)) for a, b in zip(grads, outs))
+
+
+@pytest.mark.parametrize("count", [999, 1000, 1001, 2500])
+def test_more_tensors_than_one_launch_takes(count):
+    sizes = [1 + (7 * i) % 40 for i in range(count)]
+    grads = tensors(count, sizes)
+    outs = [torch.full_like(g, NAN) for g in grads]
+    check(grads, outs, 3.0)
+
+
+def test_same_bits_every_time_and_on_another_stream():
+    grads = tensors(5, [300001, 77, 49152])
+    outs = [torch.empty_like(g) for g in grads]
+    first = run(list(zip(grads, outs)), 1.0)
+    keep = [o.clone() for o in outs]
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for o in outs:
+                o.zero_()
+            assert run(list(zip(grads, outs)), 1.0) == first
+        assert all(torch.equal(a, b) for a, b in zip(keep, outs))
+
+
+def test_follows_the_gradients_in_stream_order():
+    """The clip right behind the kernels that write the gradients, several times over: no stale norm."""
+    g = torch.ones(100000, device="cuda")
+    norms = torch.empty(20, device="cuda")
+    arr = lora.make_grads([(g, g)])
+    ws = G.workspace(lora.lora_clip_workspace_size(arr))
+    for i in range(20):
+        g.fill_(float(i + 1))
+        lora.lora_clip_grads(arr, 1.0, norms[i:], None, ws, ws.numel())
+    torch.cuda.synchronize()
+    want = torch.arange(1, 21, device="cuda") * math.sqrt(100000)
+    assert torch.allclose(norms, want, rtol=2e-6)
+    assert torch.allclose(g, torch.full_like(g, 1 / math.sqrt(100000)), rtol=4e-6)
+
+
+def test_tensor_past_two_to_the_31_elements():
+    n = (1 << 31) + 77
+    g = torch.full((n,), 2.0, dtype=torch.bfloat16, device="cuda")
+    norm, coef = run([(g, g)], math.sqrt(n))
+    assert norm == pytest.approx(2.0 * math.sqrt(n), rel=2e-6) and coef == pytest.approx(0.5, rel=2e-6)
+    assert (g[:100] == 1).all() and (g[-100:] == 1).all() and float(g[::4096].float().sum()) == g[::4096].numel()
