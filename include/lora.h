@@ -308,8 +308,9 @@ int lora_decode_q4(const lora_proj* projs, int n_proj, void* workspace, size_t w
  * sequence i is [offsets[i], offsets[i+1]); offsets ascend from 0 to T
  * (checked on the device: lora_read_status then reports LORA_EINVAL and the
  * outputs are unspecified); a sequence may be empty.  Tokens with mask 0 take no
- * part: nothing of them is read but the mask, and their derivative is zero.
- * The sums over tokens are held in fp64, in a fixed order.
+ * part, whatever their other values are, and their derivative is zero.  The
+ * sums over tokens are held in more than fp32 (pairs of fp32, then fp64), in an order
+ * that depends on the sizes only.
  * Arrays of one value per token, sequence or pair need the alignment of their
  * type only; dh_nll and dh 16 bytes, and d a multiple of 8.  dh may be dh_nll
  * (scaled in place); dh NULL: no gradient of the hidden states.

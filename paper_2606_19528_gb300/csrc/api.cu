@@ -2126,13 +2126,14 @@ int decode_check_ptrs(const lora_proj& p) {
 }
 
 struct ObjectivePlan {
-  size_t seq = 0, u = 0, total = 0;
+  size_t seq = 0, n = 0, u = 0, total = 0;
 };
 
 int objective_plan(int64_t T, int64_t groups, int64_t d, ObjectivePlan* pl) {
   if (T < 1 || T > (1ll << 24) || groups < 1 || groups > (1ll << 24) || d < 8 || d % 8 || d > (1ll << 20))
     return LORA_EINVAL;
-  pl->u = up256((size_t)groups * sizeof(ObjectiveSeq));
+  pl->n = up256((size_t)groups * sizeof(ObjectiveSeq));
+  pl->u = pl->n + up256((size_t)groups * sizeof(int));
   pl->total = pl->u + up256((size_t)T * sizeof(float));
   return LORA_OK;
 }
@@ -2168,14 +2169,14 @@ int pref_check(const lora_pref_args* a, ObjectivePlan* pl) {
 }
 
 // Runs `launch(batch, first partial sum, CTAs)` over the tensors in batches that fit a launch's table (the tensors
-// without elements left out); *partials: the batches' partial sums together.  Planned for kPlanSms SMs.
+// without elements left out; without any, one empty batch); *partials: the batches' partial sums together.  Planned
+// for kPlanSms SMs.
 template <typename Launch>
 int clip_batches(const lora_grad* grads, int n, int* partials, Launch launch) {
   ClipBatch b;
   b.n = b.chunks = 0;
   *partials = 0;
   auto flush = [&]() -> int {
-    if (!b.n) return LORA_OK;
     const int ctas = clip_ctas(b.chunks, kPlanSms);
     const int rc = launch(b, *partials, ctas);
     *partials += ctas;
@@ -2186,7 +2187,7 @@ int clip_batches(const lora_grad* grads, int n, int* partials, Launch launch) {
   for (int i = 0; i < n; ++i) {
     const lora_grad& g = grads[i];
     if (!g.n) continue;
-    const int chunks = cdiv(g.n, kClipChunk);  // at most 2^25
+    const int chunks = cdiv(g.n, kClipChunk);  // at most 2^28
     if ((b.n == kClipTensors || b.chunks > (1 << 30)) && (rc = flush()) != LORA_OK) return rc;
     ClipTensor& t = b.t[b.n++];
     t.src = g.src;
@@ -2196,7 +2197,7 @@ int clip_batches(const lora_grad* grads, int n, int* partials, Launch launch) {
     t.half = g.dtype == LORA_BF16;
     b.chunks += chunks;
   }
-  return flush();
+  return b.n || !*partials ? flush() : LORA_OK;
 }
 
 int clip_check(const lora_grad* grads, int n, size_t* bytes) {
@@ -2741,6 +2742,7 @@ int lora_policy_fwd_bwd(const lora_policy_args* a, void* workspace, size_t works
   o.T = (int)a->T;
   o.groups = (int)a->S;
   o.d = (int)a->d;
+  o.policy = 1;
   o.per_token = a->advantage_per_token != 0;
   o.reduction = a->reduction;
   o.clip_low = a->clip_low;
@@ -2755,6 +2757,7 @@ int lora_policy_fwd_bwd(const lora_policy_args* a, void* workspace, size_t works
   o.token_weight = a->token_weight;
   o.dh = mb(a->dh);
   o.seq = at<ObjectiveSeq>(workspace, pl.seq);
+  o.n = at<int>(workspace, pl.n);
   o.u = at<float>(workspace, pl.u);
   o.status = d->status;
   return rec(launch_policy(o, d->num_sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LORA_OK : LORA_ECUDA);
@@ -2798,6 +2801,7 @@ int lora_pref_fwd_bwd(const lora_pref_args* a, void* workspace, size_t workspace
   o.token_weight = a->token_weight;
   o.dh = mb(a->dh);
   o.seq = at<ObjectiveSeq>(workspace, pl.seq);
+  o.n = at<int>(workspace, pl.n);
   o.u = at<float>(workspace, pl.u);
   o.status = d->status;
   return rec(launch_pref(o, d->num_sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LORA_OK : LORA_ECUDA);
@@ -2823,20 +2827,20 @@ int lora_clip_grads(const lora_grad* grads, int n_grads, float max_norm, float* 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   double* partial = at<double>(workspace, 0);
   int partials = 0, again = 0;
+  const bool one_batch = n_grads <= kClipTensors;
+  bool done = false;
   rc = clip_batches(grads, n_grads, &partials, [&](const ClipBatch& b, int first, int ctas) {
-    return launch_clip_sum(b, partial + first, ctas, st) == cudaSuccess ? LORA_OK : LORA_ECUDA;
+    done = one_batch && clip_is_small(b);
+    return (done ? launch_clip_one(b, max_norm, norm, coef, st) : launch_clip_sum(b, partial + first, ctas, st)) ==
+                   cudaSuccess
+               ? LORA_OK
+               : LORA_ECUDA;
   });
-  if (rc != LORA_OK) return rec(rc);
-  auto scale = [&](const ClipBatch& b, int, int ctas) {
+  if (rc != LORA_OK || done) return rec(rc);
+  return rec(clip_batches(grads, n_grads, &again, [&](const ClipBatch& b, int, int ctas) {
     return launch_clip_scale(b, partial, partials, max_norm, norm, coef, ctas, st) == cudaSuccess ? LORA_OK
                                                                                                   : LORA_ECUDA;
-  };
-  if (partials == 0) {  // no element: norm 0
-    ClipBatch b;
-    b.n = b.chunks = 0;
-    return rec(scale(b, 0, 1));
-  }
-  return rec(clip_batches(grads, n_grads, &again, scale));
+  }));
 }
 
 int lora_wait_selftest(int64_t limit_ns, void* stream) {

@@ -420,9 +420,9 @@ struct DecodeBatch {
 cudaError_t launch_decode(DecodeBatch& b, int num_sms, cudaStream_t stream);
 
 // ---------------------------------------------------------------- policy and preference losses
-struct ObjectiveSeq {  // what the first launch leaves per sequence (policy) or pair (preference)
-  double loss, kl;
-  int n, clipped;
+struct ObjectiveSeq {  // what the first launch leaves per sequence (policy) or pair (preference), sums as fp32 pairs
+  float loss_hi, loss_lo, kl_hi, kl_lo;
+  int clipped;
 };
 
 struct Objective {
@@ -431,6 +431,7 @@ struct Objective {
   const float *nll, *old_nll, *ref_nll, *adv;
   const uint8_t* mask;
   int T, groups, d;  // groups: sequences (policy) or pairs (preference)
+  int policy;           // 1: policy, 0: preference
   // policy
   int per_token, reduction;
   float clip_low, clip_high, log_low, log_high, beta, scale;
@@ -443,7 +444,8 @@ struct Objective {
   __nv_bfloat16* dh;
   // workspace
   ObjectiveSeq* seq;  // [groups]
-  float* u;           // [T]: the tokens' weights, but for the factor 1 / (trainable tokens)
+  int* n;             // [groups]: trainable tokens
+  float* u;           // [T]: the tokens' weights, but for the factor 1 / (trainable tokens of the batch)
   int* status;
 };
 cudaError_t launch_policy(const Objective& o, int num_sms, cudaStream_t stream);
@@ -454,11 +456,11 @@ struct ClipTensor {
   const void* src;
   void* dst;  // null: counted, not written
   long long n;
-  int chunk_begin;  // first of its chunks in the launch's list
+  int chunk_begin;  // first of its pieces in the launch's list
   int half;         // 1: bf16, 0: fp32
 };
 constexpr int kClipTensors = 1000;  // per launch: the table is a kernel argument, at most 32764 bytes
-constexpr int kClipChunk = 8192;    // elements
+constexpr int kClipChunk = 1024;    // elements of a piece
 
 struct ClipBatch {
   ClipTensor t[kClipTensors];
@@ -470,5 +472,8 @@ cudaError_t launch_clip_sum(const ClipBatch& b, double* partial, int ctas, cudaS
 // dst = src min(1, max_norm / norm) over the batch, norm from partial[0 .. n_partial).
 cudaError_t launch_clip_scale(const ClipBatch& b, const double* partial, int n_partial, float max_norm, float* norm,
                               float* coef, int ctas, cudaStream_t stream);
+// Both in one launch, where the call is one batch that clip_is_small().
+bool clip_is_small(const ClipBatch& b);
+cudaError_t launch_clip_one(const ClipBatch& b, float max_norm, float* norm, float* coef, cudaStream_t stream);
 
 }  // namespace lora

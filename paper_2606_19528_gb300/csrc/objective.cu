@@ -1,9 +1,13 @@
 // Losses over sequences of sampled or preferred tokens, from the tokens' negative log-probabilities:
-//   policy_kernel  clipped policy loss with a KL term, one block per sequence
-//   pref_kernel    loss of a chosen against a rejected sequence, one block per pair
+//   policy_kernel  clipped policy loss with a KL term, one cluster of 1 or 8 CTAs per sequence
+//   pref_kernel    loss of a chosen against a rejected sequence, one cluster per pair
 //   rows_kernel    the loss's sum, the tokens' weights w_t = d loss / d nll_t, and dh_t = w_t * d nll_t / d h_t
 // The first launch reads a few bytes per token; the second streams two rows of d bf16 per token and is bound by
-// memory.  It needs the first one's sums: a weight depends on its whole sequence or batch.
+// memory.  It needs the first one's sums (a weight depends on its whole sequence or batch), but starts beside it: its
+// first rows are on their way when the sums arrive.
+//
+// FP64 is scarce on this GPU (about 2 operations a clock and SM).  Sums over tokens are held as unevaluated pairs of
+// fp32 (a two-sum per term: 48 bits), so that only a handful of values per sequence is added in fp64.
 #include <math.h>
 
 #include <algorithm>
@@ -15,20 +19,88 @@
 namespace lora {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxCluster = 8;
+constexpr int kBatch = 4;  // tokens of a thread whose loads are in flight together
 
-template <typename T>
-__device__ T block_sum(T v) {
-  __shared__ T part[kThreads / 32];
+// hi + lo, |lo| small against hi; x is added with its rounding error (two-sum).
+struct Pair {
+  float hi = 0.f, lo = 0.f;
+  __device__ __forceinline__ void add(float x) {
+    const float s = hi + x, b = s - hi;
+    lo += (hi - (s - b)) + (x - b);
+    hi = s;
+  }
+  __device__ __forceinline__ void add(const Pair& p) {
+    add(p.hi);
+    lo += p.lo;
+  }
+  // an infinite or undefined sum has no error term
+  __device__ __forceinline__ double value() const { return isfinite(hi) ? (double)hi + (double)lo : (double)hi; }
+};
+
+__device__ __forceinline__ Pair warp_sum(Pair p) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-  __syncthreads();
-  T s = 0;
+  for (int o = 16; o > 0; o >>= 1) {
+    Pair q;
+    q.hi = __shfl_xor_sync(0xffffffffu, p.hi, o);
+    q.lo = __shfl_xor_sync(0xffffffffu, p.lo, o);
+    p.add(q);
+  }
+  return p;
+}
+
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t n;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+  return n;
+}
+
+// Two sums and two counts over the cluster's threads.
+struct Totals {
+  Pair a, b;
+  int n, m;
+};
+
+// Every thread of the cluster gets the sums over it, added in the order of the warps: each warp's go into its slot
+// of every CTA's shared memory.
+__device__ __forceinline__ Totals cluster_totals(Totals v, Totals* slots) {
+  const uint32_t ctas = cluster_size(), rank = ctas > 1 ? cluster_ctarank() : 0;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  v.a = warp_sum(v.a);
+  v.b = warp_sum(v.b);
+  v.n = __reduce_add_sync(0xffffffffu, v.n);
+  v.m = __reduce_add_sync(0xffffffffu, v.m);
+  if (lane < (int)ctas) {
+    const uint32_t words[6] = {__float_as_uint(v.a.hi), __float_as_uint(v.a.lo), __float_as_uint(v.b.hi),
+                               __float_as_uint(v.b.lo), (uint32_t)v.n,           (uint32_t)v.m};
+    const uint32_t at = smem_u32(&slots[rank * kWarps + warp]);
+    if (ctas > 1) {
+      const uint32_t to = mapa_shared(at, lane);
 #pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) s += part[w];
-  return s;
+      for (int i = 0; i < 6; ++i) st_cluster_u32(to + 4 * i, words[i]);
+    } else {
+      slots[warp] = v;
+    }
+  }
+  if (ctas > 1)
+    cluster_sync_all();
+  else
+    __syncthreads();
+  Totals t;
+  t.n = t.m = 0;
+  for (int s = lane; s < (int)ctas * kWarps; s += 32) {
+    const Totals& q = slots[s];
+    t.a.add(q.a);
+    t.b.add(q.b);
+    t.n += q.n;
+    t.m += q.m;
+  }
+  t.a = warp_sum(t.a);
+  t.b = warp_sum(t.b);
+  t.n = __reduce_add_sync(0xffffffffu, t.n);
+  t.m = __reduce_add_sync(0xffffffffu, t.m);
+  return t;
 }
 
 // Offsets i and i + 1, inside [0, T] and in order whatever the array holds; records ones that are not.
@@ -50,166 +122,342 @@ __device__ __forceinline__ float exp_minus_line(float e) {
 }
 
 __global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant__ Objective o) {
+  __shared__ Totals slots[kMaxCluster * kWarps];
+  const int ctas = (int)cluster_size(), s = (int)blockIdx.x / ctas;
   griddep_wait();
   griddep_launch_dependents();
-  const int s = blockIdx.x;
   int lo, hi;
   range(o, s, o.groups - 1, &lo, &hi);
-  int n = 0;
-  for (int t = lo + threadIdx.x; t < hi; t += kThreads) n += !o.mask || o.mask[t] ? 1 : 0;
-  n = block_sum(n);
-  const double norm = (double)o.scale * (o.reduction == LORA_MEAN_SEQS && n ? 1.0 / ((double)o.groups * n) : 1.0);
-  double loss = 0.0, kl_sum = 0.0;
-  int clips = 0;
-  for (int t = lo + threadIdx.x; t < hi; t += kThreads) {
-    float u = 0.f;
-    if (!o.mask || o.mask[t]) {
-      const float nll = o.nll[t], delta = o.old_nll[t] - nll, A = o.adv[o.per_token ? t : s];
-      const bool up = A > 0.f && delta > o.log_high, down = A < 0.f && delta < o.log_low;
-      float l;
-      if (up || down) {
-        l = -A * (up ? 1.f + o.clip_high : 1.f - o.clip_low);
-        ++clips;
-      } else {
-        u = A * expf(delta);
-        l = -u;
-      }
-      loss += (double)l;
-      if (o.ref_nll) {
-        const float e = nll - o.ref_nll[t], kl = exp_minus_line(e);
-        loss += (double)o.beta * kl;
-        kl_sum += (double)kl;
-        u = fmaf(o.beta, expm1f(e), u);
-      }
-      u *= (float)norm;
+  const bool by_seq = o.reduction == LORA_MEAN_SEQS;
+  const int stride = ctas * kThreads, first = lo + ((int)blockIdx.x % ctas) * kThreads + (int)threadIdx.x;
+  const bool one_batch = hi - lo <= kBatch * stride;
+  const float adv_seq = o.per_token ? 0.f : o.adv[s];
+  Totals v;
+  v.n = v.m = 0;
+  float u[kBatch];
+  for (int t0 = first; t0 < hi; t0 += kBatch * stride) {
+    float nll[kBatch], old[kBatch], ref[kBatch], adv[kBatch];
+    bool on[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int t = t0 + k * stride;
+      const int at = min(t, hi - 1);  // a masked token's values are loaded with its mask, and dropped
+      on[k] = t < hi && (!o.mask || o.mask[at]);
+      nll[k] = o.nll[at];
+      old[k] = o.old_nll[at];
+      ref[k] = o.ref_nll ? o.ref_nll[at] : 0.f;
+      adv[k] = o.per_token ? o.adv[at] : adv_seq;
     }
-    o.u[t] = u;
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      u[k] = 0.f;
+      if (on[k]) {
+        const float delta = old[k] - nll[k], A = adv[k];
+        const bool up = A > 0.f && delta > o.log_high, down = A < 0.f && delta < o.log_low;
+        float l;
+        if (up || down) {
+          l = -A * (up ? 1.f + o.clip_high : 1.f - o.clip_low);
+          ++v.m;
+        } else {
+          u[k] = A * expf(delta);
+          l = -u[k];
+        }
+        if (o.ref_nll) {
+          const float e = nll[k] - ref[k], kl = exp_minus_line(e);
+          v.b.add(kl);
+          u[k] = fmaf(o.beta, expm1f(e), u[k]);
+        }
+        v.a.add(l);
+        ++v.n;
+        u[k] *= o.scale;
+      }
+      if (t0 + k * stride < hi && (!by_seq || !one_batch)) o.u[t0 + k * stride] = u[k];
+    }
   }
-  loss = block_sum(loss);
-  kl_sum = block_sum(kl_sum);
-  clips = block_sum(clips);
-  if (threadIdx.x == 0) o.seq[s] = ObjectiveSeq{loss * norm, kl_sum, n, clips};
+  const Totals all = cluster_totals(v, slots);
+  if (by_seq && all.n) {
+    const float norm = 1.f / ((float)o.groups * (float)all.n);
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) u[k] *= norm;  // of the only batch
+    if (one_batch) {
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k)
+        if (first + k * stride < hi) o.u[first + k * stride] = u[k];
+    } else {
+      for (int t = first; t < hi; t += stride) o.u[t] *= norm;
+    }
+  } else if (by_seq) {  // no trainable token
+    for (int t = first; t < hi; t += stride) o.u[t] = 0.f;
+  }
+  if (blockIdx.x % ctas == 0 && threadIdx.x == 0) {
+    o.n[s] = all.n;
+    o.seq[s] = ObjectiveSeq{all.a.hi, all.a.lo, all.b.hi, all.b.lo, all.m};
+  }
+}
+
+// e^-m for m >= 0 given as a double: the part that fp32 drops of m is a factor near 1.
+__device__ __forceinline__ float exp_neg(double m) {
+  if (m > 200.0) return 0.f;
+  const float hi = (float)m;
+  return expf(-hi) * (1.f - (float)(m - (double)hi));
 }
 
 __global__ void __launch_bounds__(kThreads) pref_kernel(const __grid_constant__ Objective o) {
+  __shared__ Totals slots[kMaxCluster * kWarps];
+  __shared__ float s_w[2];
+  const int ctas = (int)cluster_size(), p = (int)blockIdx.x / ctas, rank = (int)blockIdx.x % ctas;
   griddep_wait();
   griddep_launch_dependents();
-  const int p = blockIdx.x;
   int lo[2], hi[2];
   range(o, 2 * p, 2 * o.groups - 1, &lo[0], &hi[0]);
   range(o, 2 * p + 1, 2 * o.groups - 1, &lo[1], &hi[1]);
-  double R[2];
-  double share[2];
-  for (int c = 0; c < 2; ++c) {
-    double sum = 0.0;
-    int n = 0;
-    for (int t = lo[c] + threadIdx.x; t < hi[c]; t += kThreads) {
-      if (o.mask && !o.mask[t]) continue;
-      sum += (o.ref_nll ? (double)o.ref_nll[t] : 0.0) - (double)o.nll[t];
-      ++n;
+  const int stride = ctas * kThreads, first = rank * kThreads + (int)threadIdx.x;
+  const int n0 = hi[0] - lo[0], n1 = hi[1] - lo[1];
+  // position i of the pair: the first sequence's tokens, then the second's
+  auto token = [&](int i) { return i < n0 ? lo[0] + i : lo[1] + i - n0; };
+  Totals v;
+  v.n = v.m = 0;
+  const int total = n0 + n1;
+  for (int i0 = first; i0 < total; i0 += kBatch * stride) {
+    float nll[kBatch], ref[kBatch];
+    bool on[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int i = i0 + k * stride, t = token(min(i, total - 1));
+      on[k] = i < total && (!o.mask || o.mask[t]);
+      nll[k] = o.nll[t];
+      ref[k] = o.ref_nll ? o.ref_nll[t] : 0.f;
     }
-    sum = block_sum(sum);
-    n = block_sum(n);
-    share[c] = o.mean_tokens && n ? 1.0 / n : 1.0;
-    R[c] = sum * share[c];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      if (!on[k]) continue;
+      Pair& sum = i0 + k * stride < n0 ? v.a : v.b;
+      sum.add(ref[k]);
+      sum.add(-nll[k]);
+      ++(i0 + k * stride < n0 ? v.n : v.m);
+    }
   }
-  const double beta = o.beta, m = beta * (R[0] - R[1]) - (double)o.margin;
-  double loss, slope;
-  if (o.kind == LORA_PREF_SIGMOID) {
-    const double ls = o.smoothing, tail = log1p(exp(-fabs(m)));
-    loss = (1.0 - ls) * (tail + fmax(-m, 0.0)) + ls * (tail + fmax(m, 0.0));
-    slope = -(1.0 - ls) / (1.0 + exp(m)) + ls / (1.0 + exp(-m));
-  } else if (o.kind == LORA_PREF_HINGE) {
-    loss = fmax(1.0 - m, 0.0);
-    slope = m < 1.0 ? -1.0 : 0.0;
-  } else {
-    loss = (m - 0.5) * (m - 0.5) / (beta * beta);
-    slope = 2.0 * (m - 0.5) / (beta * beta);
-  }
-  const double norm = (double)o.scale / o.groups;
-  for (int c = 0; c < 2; ++c) {
-    const float w = (float)((c ? slope : -slope) * beta * norm * share[c]);
-    for (int t = lo[c] + threadIdx.x; t < hi[c]; t += kThreads) o.u[t] = o.mask && !o.mask[t] ? 0.f : w;
-  }
+  const Totals all = cluster_totals(v, slots);
   if (threadIdx.x == 0) {
-    o.seq[p] = ObjectiveSeq{loss * norm, 0.0, 0, 0};
-    if (o.rewards) {
-      o.rewards[2 * p] = (float)(beta * R[0]);
-      o.rewards[2 * p + 1] = (float)(beta * R[1]);
+    const double share0 = o.mean_tokens && all.n ? 1.0 / all.n : 1.0;
+    const double share1 = o.mean_tokens && all.m ? 1.0 / all.m : 1.0;
+    const double beta = o.beta, r0 = beta * (all.a.value() * share0), r1 = beta * (all.b.value() * share1);
+    const double m = r0 - r1 - (double)o.margin;
+    double loss, slope;
+    if (o.kind == LORA_PREF_SIGMOID) {
+      // with e = exp(-|m|): log(1 + exp(-|m|)), and the smaller and the larger of sigmoid(+-m)
+      const float e = exp_neg(fabs(m)), small = e / (1.f + e), large = 1.f / (1.f + e);
+      const double tail = (double)log1pf(e), ls = o.smoothing, by = m < 0.0 ? -(1.0 - ls) : ls;
+      loss = tail + (by != 0.0 ? by * m : 0.0);
+      slope = m < 0.0 ? ls * (double)small - (1.0 - ls) * (double)large
+                      : ls * (double)large - (1.0 - ls) * (double)small;
+    } else if (o.kind == LORA_PREF_HINGE) {
+      loss = m < 1.0 ? 1.0 - m : (m != m ? m : 0.0);
+      slope = m < 1.0 ? -1.0 : (m != m ? m : 0.0);
+    } else {
+      const double x = (m - 0.5) / beta;
+      loss = x * x;
+      slope = 2.0 * x / beta;
     }
+    const double norm = (double)o.scale / o.groups, w = slope * beta * norm;
+    s_w[0] = (float)(-w * share0);
+    s_w[1] = (float)(w * share1);
+    if (rank == 0) {
+      loss *= norm;
+      const float l = (float)loss;
+      o.seq[p] = ObjectiveSeq{l, isfinite(l) ? (float)(loss - (double)l) : 0.f, 0.f, 0.f, 0};
+      o.n[p] = all.n + all.m;
+      if (o.rewards) {
+        o.rewards[2 * p] = (float)r0;
+        o.rewards[2 * p + 1] = (float)r1;
+      }
+    }
+  }
+  __syncthreads();
+  for (int i = first; i < total; i += stride) {
+    const int t = token(i);
+    o.u[t] = o.mask && !o.mask[t] ? 0.f : s_w[i < n0 ? 0 : 1];
   }
 }
 
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// The loss and the statistics, by one block, in a fixed order.
+__device__ void finish(const Objective& o) {
+  __shared__ double part[3][kWarps];
+  __shared__ long long clips[kWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const bool by_seq = o.reduction == LORA_MEAN_SEQS;
+  double loss = 0.0, kl = 0.0, n = 0.0;
+  long long c = 0;
+  for (int s = threadIdx.x; s < o.groups; s += kThreads) {
+    const ObjectiveSeq q = o.seq[s];
+    const int tokens = o.n[s];
+    Pair l, k;
+    l.hi = q.loss_hi, l.lo = q.loss_lo, k.hi = q.kl_hi, k.lo = q.kl_lo;
+    const double kv = k.value(), lv = l.value() + (o.policy && o.ref_nll ? (double)o.beta * kv : 0.0);
+    loss += by_seq && tokens ? lv / tokens : lv;
+    kl += kv;
+    n += (double)tokens;
+    c += q.clipped;
+  }
+  loss = warp_sum(loss);
+  kl = warp_sum(kl);
+  n = warp_sum(n);
+#pragma unroll
+  for (int i = 16; i > 0; i >>= 1) c += __shfl_xor_sync(0xffffffffu, c, i);
+  if (lane == 0) {
+    part[0][warp] = loss;
+    part[1][warp] = kl;
+    part[2][warp] = n;
+    clips[warp] = c;
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  const int used = min(kWarps, (o.groups + 31) / 32);
+  for (int w = 1; w < used; ++w) {
+    loss += part[0][w];
+    kl += part[1][w];
+    n += part[2][w];
+    c += clips[w];
+  }
+  const double per = n > 0.0 ? 1.0 / n : 0.0;
+  if (o.reduction == LORA_MEAN_TOKENS) loss *= per;
+  if (by_seq) loss /= o.groups;
+  *o.loss = (float)(o.policy ? loss * (double)o.scale : loss);
+  if (o.stats) {
+    o.stats[0] = (float)(kl * per);
+    o.stats[1] = (float)((double)c * per);
+  }
+}
+
+// Trainable tokens of the batch; every thread gets it.
+__device__ __forceinline__ long long count_tokens(const Objective& o) {
+  __shared__ long long part[kWarps];
+  long long n = 0;
+  for (int s = threadIdx.x; s < o.groups; s += kThreads) n += o.n[s];
+#pragma unroll
+  for (int i = 16; i > 0; i >>= 1) n += __shfl_xor_sync(0xffffffffu, n, i);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = n;
+  __syncthreads();
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) n += part[w];
+  return n;
+}
+
+// Block 0 finishes the loss.  The others' warps take parts of rows: four 16-byte vectors a lane, the next part's
+// loads issued before this one is written, the weight of the one after that on its way.
+constexpr int kVecs = 4;
+
 __global__ void __launch_bounds__(kThreads) rows_kernel(const __grid_constant__ Objective o) {
+  if (blockIdx.x == 0) {
+    griddep_wait();
+    griddep_launch_dependents();
+    finish(o);
+    return;
+  }
+  const int lane = threadIdx.x & 31, vecs = o.dh ? o.d / 8 : 0;
+  const int parts = o.dh ? (vecs + 32 * kVecs - 1) / (32 * kVecs) : 1;
+  const int warps = ((int)gridDim.x - 1) * kWarps, w0 = ((int)blockIdx.x - 1) * kWarps + (int)(threadIdx.x >> 5);
+  const int dt = warps / parts, dp = warps % parts;
+  struct At {
+    int t, part;
+  };
+  auto next = [&](At a) {
+    a.t += dt;
+    a.part += dp;
+    if (a.part >= parts) {
+      a.part -= parts;
+      ++a.t;
+    }
+    return a;
+  };
+  uint4 q[kVecs];
+  auto fetch = [&](At a, bool wanted) {
+    const uint4* src = reinterpret_cast<const uint4*>(o.dh_nll + (long long)a.t * o.d);
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      const int v = (a.part * kVecs + k) * 32 + lane;
+      q[k] = wanted && v < vecs ? __ldcs(src + v) : make_uint4(0u, 0u, 0u, 0u);
+    }
+  };
+  At a{w0 / parts, w0 % parts};
+  // the mask and the rows were written before the first launch of the call began
+  fetch(a, o.dh && a.t < o.T && (!o.mask || o.mask[a.t]));
   griddep_wait();
   griddep_launch_dependents();
+  At b = next(a);
+  float ua = a.t < o.T ? o.u[a.t] : 0.f, ub = b.t < o.T ? o.u[b.t] : 0.f;
   float inv = 1.f;
-  double total = 1.0;
-  const bool by_tokens = o.reduction == LORA_MEAN_TOKENS;
-  if (by_tokens || blockIdx.x == 0) {
-    long long n = 0;
-    for (int s = threadIdx.x; s < o.groups; s += kThreads) n += o.seq[s].n;
-    total = (double)block_sum(n);
-    if (by_tokens && total > 0.0) inv = (float)(1.0 / total);
+  if (o.reduction == LORA_MEAN_TOKENS) {
+    const long long n = count_tokens(o);
+    inv = n ? 1.f / (float)n : 1.f;
   }
-  if (blockIdx.x == 0) {
-    double loss = 0.0, kl = 0.0;
-    long long clips = 0;
-    for (int s = threadIdx.x; s < o.groups; s += kThreads) {
-      loss += o.seq[s].loss;
-      kl += o.seq[s].kl;
-      clips += o.seq[s].clipped;
-    }
-    loss = block_sum(loss);
-    kl = block_sum(kl);
-    clips = block_sum(clips);
-    if (threadIdx.x == 0) {
-      const double per = total > 0.0 ? 1.0 / total : 0.0;
-      *o.loss = (float)(by_tokens ? loss * per : loss);
-      if (o.stats) {
-        o.stats[0] = (float)(kl * per);
-        o.stats[1] = (float)((double)clips * per);
-      }
-    }
-  }
-  if (!o.dh && !o.token_weight) return;
-  const int lane = threadIdx.x & 31, vecs = o.d / 8;
-  for (int t = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); t < o.T; t += gridDim.x * (kThreads / 32)) {
-    const float w = o.u[t] * inv;
-    if (o.token_weight && lane == 0) o.token_weight[t] = w;
-    if (!o.dh) continue;
-    const uint4* src = reinterpret_cast<const uint4*>(o.dh_nll + (long long)t * o.d);
-    uint4* dst = reinterpret_cast<uint4*>(o.dh + (long long)t * o.d);
-    for (int v = lane; v < vecs; v += 32) {
-      uint4 r = make_uint4(0u, 0u, 0u, 0u);
-      if (w != 0.f) {  // also a NaN; a row of weight zero is zero whatever the row holds
-        const uint4 q = src[v];
-        const uint32_t in[4] = {q.x, q.y, q.z, q.w};
-        uint32_t out[4];
+  while (a.t < o.T) {
+    const float w = ua * inv;
+    uint4 r[kVecs];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          out[e] = pack_bf16x2(w * __uint_as_float(in[e] << 16), w * __uint_as_float(in[e] & 0xffff0000u));
-        r = make_uint4(out[0], out[1], out[2], out[3]);
+    for (int k = 0; k < kVecs; ++k) r[k] = q[k];
+    fetch(b, o.dh && ub != 0.f);  // also a NaN
+    const At c = next(b);
+    const float uc = c.t < o.T ? o.u[c.t] : 0.f;
+    if (o.token_weight && a.part == 0 && lane == 0) o.token_weight[a.t] = w;
+    if (o.dh) {
+      uint4* dst = reinterpret_cast<uint4*>(o.dh + (long long)a.t * o.d);
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        const int v = (a.part * kVecs + k) * 32 + lane;
+        if (v >= vecs) continue;
+        uint4 out = make_uint4(0u, 0u, 0u, 0u);
+        if (ua != 0.f) {  // a row of weight zero is zero whatever it holds
+          const uint32_t in[4] = {r[k].x, r[k].y, r[k].z, r[k].w};
+          uint32_t x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            x[e] = pack_bf16x2(w * __uint_as_float(in[e] << 16), w * __uint_as_float(in[e] & 0xffff0000u));
+          out = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+        __stcs(dst + v, out);
       }
-      dst[v] = r;
     }
+    a = b;
+    b = c;
+    ua = ub;
+    ub = uc;
   }
+}
+
+// Tokens of a group at which its CTA would take more than two batches: eight of them share it then.
+int cluster_for(const Objective& o, int num_sms) {
+  const long long per = (long long)o.T / o.groups;
+  return per > 2 * kBatch * kThreads && o.groups * kMaxCluster <= 8 * num_sms ? kMaxCluster : 1;
 }
 
 cudaError_t launch_rows(const Objective& o, int num_sms, cudaStream_t st) {
-  const int ctas = o.dh || o.token_weight ? std::min((o.T + 7) / 8, 8 * num_sms) : 1;
-  return launch_kernel(rows_kernel, dim3(ctas), dim3(kThreads), 0, st, 1, o);
+  int ctas = 0;
+  if (o.dh || o.token_weight) {
+    const long long parts = o.dh ? (o.d / 8 + 32 * kVecs - 1) / (32 * kVecs) : 1;
+    ctas = (int)std::min<long long>((o.T * parts + kWarps - 1) / kWarps, 4 * num_sms);
+  }
+  return launch_kernel(rows_kernel, dim3(1 + ctas), dim3(kThreads), 0, st, 1, o);
 }
 
 }  // namespace
 
 cudaError_t launch_policy(const Objective& o, int num_sms, cudaStream_t st) {
-  const cudaError_t e = launch_kernel(policy_kernel, dim3(o.groups), dim3(kThreads), 0, st, 1, o);
+  const int c = cluster_for(o, num_sms);
+  const cudaError_t e = launch_kernel(policy_kernel, dim3(o.groups * c), dim3(kThreads), 0, st, c, o);
   return e != cudaSuccess ? e : launch_rows(o, num_sms, st);
 }
 
 cudaError_t launch_pref(const Objective& o, int num_sms, cudaStream_t st) {
-  const cudaError_t e = launch_kernel(pref_kernel, dim3(o.groups), dim3(kThreads), 0, st, 1, o);
+  const int c = cluster_for(o, num_sms);
+  const cudaError_t e = launch_kernel(pref_kernel, dim3(o.groups * c), dim3(kThreads), 0, st, c, o);
   return e != cudaSuccess ? e : launch_rows(o, num_sms, st);
 }
 

@@ -174,10 +174,25 @@ def _ptr(a):
     return a.data_ptr()
 
 
+_raw_stream = None
+
+
+def _current_stream() -> int:
+    """The current stream of the current device.  torch.cuda.current_stream() builds an object for it (3 us, as long
+    as two launches); the query below it is what PyTorch's own generated code calls."""
+    global _raw_stream
+    import torch
+    if _raw_stream is None:
+        raw, device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+        torch.cuda.init()
+        _raw_stream = (lambda: raw(device())) if raw and device else (
+            lambda: torch.cuda.current_stream().cuda_stream)
+    return _raw_stream()
+
+
 def _stream(s):
     if s is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     if isinstance(s, int):
         return s
     return s.cuda_stream
