@@ -288,7 +288,8 @@ int lora_topk_table(const lora_bf16* E, int64_t V, int64_t d, int64_t k, int32_t
  *     y = x W^T + (scale x A^T) B^T,   W[n, k] = bf16(s q + b) as lora_q4_weight
  * The weights are those the training calls use, element for element.  Sums are
  * held in fp32; scale x A^T is not rounded to bf16 here (lora_linear_fwd_q4
- * does, since its backward reads it), and y is rounded once.
+ * does, since its backward reads it), and y is rounded once.  s must be below
+ * 2^35 in magnitude (beyond, the weights come out infinite).
  * Fields read: shape, x, A, B, y, Wq (the others are ignored, but W must be
  * NULL).  Beyond the shapes of the other calls: T is 1 .. 16 and may differ
  * between projections, d_in is a multiple of 64, d_out any number from 1 on
@@ -309,8 +310,8 @@ int lora_decode_q4(const lora_proj* projs, int n_proj, void* workspace, size_t w
  * (checked on the device: lora_read_status then reports LORA_EINVAL and the
  * outputs are unspecified); a sequence may be empty.  Tokens with mask 0 take no
  * part, whatever their other values are, and their derivative is zero.  The
- * sums over tokens are held in more than fp32 (pairs of fp32, then fp64), in an order
- * that depends on the sizes only.
+ * sums over tokens are held in more than fp32 (pairs of fp32), in an order that
+ * depends on the sizes only.
  * Arrays of one value per token, sequence or pair need the alignment of their
  * type only; dh_nll and dh 16 bytes, and d a multiple of 8.  dh may be dh_nll
  * (scaled in place); dh NULL: no gradient of the hidden states.
@@ -398,9 +399,9 @@ int lora_pref_fwd_bwd(const lora_pref_args* args, void* workspace, size_t worksp
  * is a tensor of the same type: src itself (clipped in place; nothing is
  * written when coef is 1), one that overlaps no tensor of the call, or NULL
  * (the tensor counts toward the norm and is not written).  Squares are summed
- * in fp32 over a few dozen elements and in fp64 from there on (in fp64
- * throughout where fp32 would overflow or lose small values), in an order that
- * depends on the tensors' sizes only.  norm (device, [1])
+ * in fp32 over a few dozen elements and in more bits from there on, from scaled
+ * elements where fp32 would overflow or lose small ones, in an order that
+ * depends on the tensors' sizes and alignment only.  norm (device, [1])
  * and coef (device, [1], or NULL) are written.  A norm that is not finite (a
  * gradient holds an infinity or a NaN) makes coef 1: the gradients are passed
  * on as they are, and the caller sees the norm.  max_norm >= 0, infinity for

@@ -2109,7 +2109,7 @@ int decode_check(const lora_proj* projs, int n, size_t* bytes) {
     if (s.T < 1 || s.T > kDecodeMaxT || s.d_in < 64 || s.d_in % 64 || s.d_in > (1ll << 20) || s.d_out < 1 ||
         s.d_out > (1ll << 20) || s.rank < 0 || s.rank > 128 || !isfinite(s.scale))
       return LORA_EINVAL;
-    total += up256((size_t)s.T * s.rank * sizeof(float));
+    total += up256(decode_su_bytes(s.T, s.rank));
   }
   *bytes = total;
   return LORA_OK;
@@ -2187,7 +2187,7 @@ int clip_batches(const lora_grad* grads, int n, int* partials, Launch launch) {
   for (int i = 0; i < n; ++i) {
     const lora_grad& g = grads[i];
     if (!g.n) continue;
-    const int chunks = cdiv(g.n, kClipChunk);  // at most 2^28
+    const int chunks = cdiv(g.n, kClipChunk);  // at most 2^29
     if ((b.n == kClipTensors || b.chunks > (1 << 30)) && (rc = flush()) != LORA_OK) return rc;
     ClipTensor& t = b.t[b.n++];
     t.src = g.src;
@@ -2704,13 +2704,13 @@ int lora_decode_q4(const lora_proj* projs, int n_proj, void* workspace, size_t w
     p.A = cb(q.A);
     p.B = cb(q.B);
     p.y = mb(q.y);
-    p.su = at<float>(workspace, off);
+    p.su = at<uint32_t>(workspace, off);
     p.scale = q.shape.scale;
     p.T = (int)q.shape.T;
     p.N = (int)q.shape.d_out;
     p.K = (int)q.shape.d_in;
     p.r = (int)q.shape.rank;
-    off += up256((size_t)p.T * p.r * sizeof(float));
+    off += up256(decode_su_bytes(p.T, p.r));
   }
   return rec(launch_decode(b, d->num_sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LORA_OK : LORA_ECUDA);
 }

@@ -403,7 +403,7 @@ struct DecodeProj {
   const __nv_bfloat16* A;       // [r, K]
   const __nv_bfloat16* B;       // [N, r]
   __nv_bfloat16* y;             // [T, N]
-  float* su;                    // [T, r]: scale * x A^T, written by the first launch
+  uint32_t* su;                 // decode_su_bytes(T, r): scale * x A^T, written by the first launch
   float scale;
   int T, N, K, r;
   int tile_begin;  // first of its row tiles in the launch's list
@@ -413,8 +413,10 @@ struct DecodeProj {
 struct DecodeBatch {
   DecodeProj p[kDecodeMaxProjs];
   int n, tiles, rows;
+  int after_su;  // the launch follows one that computes su
 };
 
+size_t decode_su_bytes(int64_t T, int64_t r);
 // su of every projection with an adapter (nothing to launch without one), then y = x W^T + su B^T.  The caller
 // sets all but the begins and the totals.
 cudaError_t launch_decode(DecodeBatch& b, int num_sms, cudaStream_t stream);
@@ -460,7 +462,7 @@ struct ClipTensor {
   int half;         // 1: bf16, 0: fp32
 };
 constexpr int kClipTensors = 1000;  // per launch: the table is a kernel argument, at most 32764 bytes
-constexpr int kClipChunk = 1024;    // elements of a piece
+constexpr int kClipChunk = 512;     // elements of a piece
 
 struct ClipBatch {
   ClipTensor t[kClipTensors];

@@ -6,8 +6,7 @@
 // memory.  It needs the first one's sums (a weight depends on its whole sequence or batch), but starts beside it: its
 // first rows are on their way when the sums arrive.
 //
-// FP64 is scarce on this GPU (about 2 operations a clock and SM).  Sums over tokens are held as unevaluated pairs of
-// fp32 (a two-sum per term: 48 bits), so that only a handful of values per sequence is added in fp64.
+// Sums over tokens are held as pairs of fp32 (48 bits).
 #include <math.h>
 
 #include <algorithm>
@@ -15,6 +14,7 @@
 #include "common.cuh"
 #include "kernels.h"
 #include "lora.h"
+#include "pair.cuh"
 
 namespace lora {
 namespace {
@@ -22,33 +22,6 @@ namespace {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kBatch = 4;  // tokens of a thread whose loads are in flight together
-
-// hi + lo, |lo| small against hi; x is added with its rounding error (two-sum).
-struct Pair {
-  float hi = 0.f, lo = 0.f;
-  __device__ __forceinline__ void add(float x) {
-    const float s = hi + x, b = s - hi;
-    lo += (hi - (s - b)) + (x - b);
-    hi = s;
-  }
-  __device__ __forceinline__ void add(const Pair& p) {
-    add(p.hi);
-    lo += p.lo;
-  }
-  // an infinite or undefined sum has no error term
-  __device__ __forceinline__ double value() const { return isfinite(hi) ? (double)hi + (double)lo : (double)hi; }
-};
-
-__device__ __forceinline__ Pair warp_sum(Pair p) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    Pair q;
-    q.hi = __shfl_xor_sync(0xffffffffu, p.hi, o);
-    q.lo = __shfl_xor_sync(0xffffffffu, p.lo, o);
-    p.add(q);
-  }
-  return p;
-}
 
 __device__ __forceinline__ uint32_t cluster_size() {
   uint32_t n;
@@ -87,8 +60,7 @@ __device__ __forceinline__ Totals cluster_totals(Totals v, Totals* slots) {
     cluster_sync_all();
   else
     __syncthreads();
-  Totals t;
-  t.n = t.m = 0;
+  Totals t{};
   for (int s = lane; s < (int)ctas * kWarps; s += 32) {
     const Totals& q = slots[s];
     t.a.add(q.a);
@@ -132,8 +104,7 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant_
   const int stride = ctas * kThreads, first = lo + ((int)blockIdx.x % ctas) * kThreads + (int)threadIdx.x;
   const bool one_batch = hi - lo <= kBatch * stride;
   const float adv_seq = o.per_token ? 0.f : o.adv[s];
-  Totals v;
-  v.n = v.m = 0;
+  Totals v{};
   float u[kBatch];
   for (int t0 = first; t0 < hi; t0 += kBatch * stride) {
     float nll[kBatch], old[kBatch], ref[kBatch], adv[kBatch];
@@ -195,11 +166,10 @@ __global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant_
   }
 }
 
-// e^-m for m >= 0 given as a double: the part that fp32 drops of m is a factor near 1.
-__device__ __forceinline__ float exp_neg(double m) {
-  if (m > 200.0) return 0.f;
-  const float hi = (float)m;
-  return expf(-hi) * (1.f - (float)(m - (double)hi));
+// e^-|m| of a pair: what lo adds is a factor near 1.
+__device__ __forceinline__ float exp_neg_abs(const Pair& m) {
+  const float hi = fabsf(m.hi);
+  return hi > 200.f ? 0.f : expf(-hi) * (1.f + (m.hi < 0.f ? m.lo : -m.lo));
 }
 
 __global__ void __launch_bounds__(kThreads) pref_kernel(const __grid_constant__ Objective o) {
@@ -215,8 +185,7 @@ __global__ void __launch_bounds__(kThreads) pref_kernel(const __grid_constant__ 
   const int n0 = hi[0] - lo[0], n1 = hi[1] - lo[1];
   // position i of the pair: the first sequence's tokens, then the second's
   auto token = [&](int i) { return i < n0 ? lo[0] + i : lo[1] + i - n0; };
-  Totals v;
-  v.n = v.m = 0;
+  Totals v{};
   const int total = n0 + n1;
   for (int i0 = first; i0 < total; i0 += kBatch * stride) {
     float nll[kBatch], ref[kBatch];
@@ -239,37 +208,46 @@ __global__ void __launch_bounds__(kThreads) pref_kernel(const __grid_constant__ 
   }
   const Totals all = cluster_totals(v, slots);
   if (threadIdx.x == 0) {
-    const double share0 = o.mean_tokens && all.n ? 1.0 / all.n : 1.0;
-    const double share1 = o.mean_tokens && all.m ? 1.0 / all.m : 1.0;
-    const double beta = o.beta, r0 = beta * (all.a.value() * share0), r1 = beta * (all.b.value() * share1);
-    const double m = r0 - r1 - (double)o.margin;
-    double loss, slope;
+    const Pair r0 = (o.mean_tokens && all.n ? all.a.over((float)all.n) : all.a).times(o.beta);
+    const Pair r1 = (o.mean_tokens && all.m ? all.b.over((float)all.m) : all.b).times(o.beta);
+    Pair m = r0;
+    m.add(-r1.hi);
+    m.lo -= r1.lo;
+    m.add(-o.margin);
+    const float mv = m.value();
+    m.lo = isfinite(mv) ? (m.hi - mv) + m.lo : 0.f;  // lo below hi's last place again
+    m.hi = mv;
+    Pair loss{};
+    float slope;  // times beta
     if (o.kind == LORA_PREF_SIGMOID) {
       // with e = exp(-|m|): log(1 + exp(-|m|)), and the smaller and the larger of sigmoid(+-m)
-      const float e = exp_neg(fabs(m)), small = e / (1.f + e), large = 1.f / (1.f + e);
-      const double tail = (double)log1pf(e), ls = o.smoothing, by = m < 0.0 ? -(1.0 - ls) : ls;
-      loss = tail + (by != 0.0 ? by * m : 0.0);
-      slope = m < 0.0 ? ls * (double)small - (1.0 - ls) * (double)large
-                      : ls * (double)large - (1.0 - ls) * (double)small;
+      const float e = exp_neg_abs(m), small = e / (1.f + e), large = 1.f / (1.f + e);
+      const float ls = o.smoothing, by = mv < 0.f ? ls - 1.f : ls;
+      if (by != 0.f) loss = m.times(by);
+      loss.add(log1pf(e));
+      slope = o.beta * (mv < 0.f ? fmaf(ls, small, (ls - 1.f) * large) : fmaf(ls, large, (ls - 1.f) * small));
     } else if (o.kind == LORA_PREF_HINGE) {
-      loss = m < 1.0 ? 1.0 - m : (m != m ? m : 0.0);
-      slope = m < 1.0 ? -1.0 : (m != m ? m : 0.0);
+      if (!(mv >= 1.f)) {  // also undefined
+        loss = m.times(-1.f);
+        loss.add(1.f);
+      }
+      slope = mv < 1.f ? -o.beta : (mv >= 1.f ? 0.f : mv);
     } else {
-      const double x = (m - 0.5) / beta;
-      loss = x * x;
-      slope = 2.0 * x / beta;
+      Pair x = m;
+      x.add(-0.5f);
+      const float xb = x.value() / o.beta;
+      loss = x.over(o.beta).times(xb);
+      slope = 2.f * xb;
     }
-    const double norm = (double)o.scale / o.groups, w = slope * beta * norm;
-    s_w[0] = (float)(-w * share0);
-    s_w[1] = (float)(w * share1);
+    const float norm = o.scale / (float)o.groups, w = slope * norm;
+    s_w[0] = o.mean_tokens && all.n ? -w / (float)all.n : -w;
+    s_w[1] = o.mean_tokens && all.m ? w / (float)all.m : w;
     if (rank == 0) {
-      loss *= norm;
-      const float l = (float)loss;
-      o.seq[p] = ObjectiveSeq{l, isfinite(l) ? (float)(loss - (double)l) : 0.f, 0.f, 0.f, 0};
+      o.seq[p] = ObjectiveSeq{loss.hi, loss.lo, 0.f, 0.f, 0};
       o.n[p] = all.n + all.m;
       if (o.rewards) {
-        o.rewards[2 * p] = (float)r0;
-        o.rewards[2 * p + 1] = (float)r1;
+        o.rewards[2 * p] = r0.value();
+        o.rewards[2 * p + 1] = r1.value();
       }
     }
   }
@@ -280,58 +258,57 @@ __global__ void __launch_bounds__(kThreads) pref_kernel(const __grid_constant__ 
   }
 }
 
-__device__ __forceinline__ double warp_sum(double v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
 // The loss and the statistics, by one block, in a fixed order.
 __device__ void finish(const Objective& o) {
-  __shared__ double part[3][kWarps];
-  __shared__ long long clips[kWarps];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __shared__ Pair part[2][kWarps];
+  __shared__ long long counts[2][kWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, used = min(kWarps, (o.groups + 31) / 32);
   const bool by_seq = o.reduction == LORA_MEAN_SEQS;
-  double loss = 0.0, kl = 0.0, n = 0.0;
-  long long c = 0;
-  for (int s = threadIdx.x; s < o.groups; s += kThreads) {
-    const ObjectiveSeq q = o.seq[s];
-    const int tokens = o.n[s];
-    Pair l, k;
-    l.hi = q.loss_hi, l.lo = q.loss_lo, k.hi = q.kl_hi, k.lo = q.kl_lo;
-    const double kv = k.value(), lv = l.value() + (o.policy && o.ref_nll ? (double)o.beta * kv : 0.0);
-    loss += by_seq && tokens ? lv / tokens : lv;
-    kl += kv;
-    n += (double)tokens;
-    c += q.clipped;
-  }
-  loss = warp_sum(loss);
-  kl = warp_sum(kl);
-  n = warp_sum(n);
+  if (warp < used) {
+    Pair loss{}, kl{};
+    long long n = 0, c = 0;
+    for (int s = threadIdx.x; s < o.groups; s += 32 * used) {
+      const ObjectiveSeq q = o.seq[s];
+      const int tokens = o.n[s];
+      Pair l, k;
+      l.hi = q.loss_hi, l.lo = q.loss_lo, k.hi = q.kl_hi, k.lo = q.kl_lo;
+      if (o.policy && o.ref_nll) l.add(k.times(o.beta));
+      loss.add(by_seq && tokens ? l.over((float)tokens) : l);
+      kl.add(k);
+      n += tokens;
+      c += q.clipped;
+    }
+    loss = warp_sum(loss);
+    kl = warp_sum(kl);
 #pragma unroll
-  for (int i = 16; i > 0; i >>= 1) c += __shfl_xor_sync(0xffffffffu, c, i);
-  if (lane == 0) {
-    part[0][warp] = loss;
-    part[1][warp] = kl;
-    part[2][warp] = n;
-    clips[warp] = c;
+    for (int i = 16; i > 0; i >>= 1) {
+      n += __shfl_xor_sync(0xffffffffu, n, i);
+      c += __shfl_xor_sync(0xffffffffu, c, i);
+    }
+    if (lane == 0) {
+      part[0][warp] = loss;
+      part[1][warp] = kl;
+      counts[0][warp] = n;
+      counts[1][warp] = c;
+    }
   }
   __syncthreads();
   if (threadIdx.x != 0) return;
-  const int used = min(kWarps, (o.groups + 31) / 32);
+  Pair loss = part[0][0], kl = part[1][0];
+  long long n = counts[0][0], c = counts[1][0];
   for (int w = 1; w < used; ++w) {
-    loss += part[0][w];
-    kl += part[1][w];
-    n += part[2][w];
-    c += clips[w];
+    loss.add(part[0][w]);
+    kl.add(part[1][w]);
+    n += counts[0][w];
+    c += counts[1][w];
   }
-  const double per = n > 0.0 ? 1.0 / n : 0.0;
-  if (o.reduction == LORA_MEAN_TOKENS) loss *= per;
-  if (by_seq) loss /= o.groups;
-  *o.loss = (float)(o.policy ? loss * (double)o.scale : loss);
+  const float tokens = (float)max(n, 1ll);
+  if (o.reduction == LORA_MEAN_TOKENS) loss = loss.over(tokens);
+  if (by_seq || !o.policy) loss = loss.over((float)o.groups);
+  *o.loss = loss.value() * o.scale;
   if (o.stats) {
-    o.stats[0] = (float)(kl * per);
-    o.stats[1] = (float)((double)c * per);
+    o.stats[0] = kl.over(tokens).value();
+    o.stats[1] = (float)c / tokens;
   }
 }
 
@@ -432,10 +409,10 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(const __grid_constant__ 
   }
 }
 
-// Tokens of a group at which its CTA would take more than two batches: eight of them share it then.
+// Eight CTAs share a group where groups hold over a token per thread on average (the longest of an uneven batch
+// several times that, and the launch ends with it) and all CTAs run at once.
 int cluster_for(const Objective& o, int num_sms) {
-  const long long per = (long long)o.T / o.groups;
-  return per > 2 * kBatch * kThreads && o.groups * kMaxCluster <= 8 * num_sms ? kMaxCluster : 1;
+  return o.T / o.groups > kThreads && o.groups <= num_sms ? kMaxCluster : 1;
 }
 
 cudaError_t launch_rows(const Objective& o, int num_sms, cudaStream_t st) {
