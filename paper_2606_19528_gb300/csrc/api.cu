@@ -2228,6 +2228,11 @@ int clip_check_ptrs(const lora_grad* grads, int n) {
 
 void note_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
 
+bool make_codes_map(CUtensorMap* m, const void* ptr, int width, int rows, int box_width, int box_rows) {
+  return make_map_plain(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, ptr, (uint64_t)width, (uint64_t)rows, (uint64_t)width,
+                        (uint32_t)box_width, (uint32_t)box_rows, CU_TENSOR_MAP_SWIZZLE_128B) == LORA_OK;
+}
+
 // Code the calling thread's most recent entry point returned (lora_last_error).
 thread_local int t_last_error = LORA_OK;
 inline int rec(int rc) {
@@ -2694,6 +2699,8 @@ int lora_decode_q4(const lora_proj* projs, int n_proj, void* workspace, size_t w
   if ((rc = device_info(&d)) != LORA_OK) return rec(rc);
   DecodeBatch b;
   b.n = n_proj;
+  b.status = d->status;
+  b.limit_ns = g_wait_limit_ns;
   size_t off = 0;
   for (int i = 0; i < n_proj; ++i) {
     const lora_proj& q = projs[i];

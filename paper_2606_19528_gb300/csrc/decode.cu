@@ -24,11 +24,13 @@ namespace lora {
 namespace {
 
 constexpr int kTileN = 16;       // output rows of a tile: M of the MMA
-constexpr int kChunk = 128;      // columns of a warp's step: two 64-wide groups, 32 columns a lane
+constexpr int kPanel = 256;      // columns of a warp's step: a 64-wide group to each of the four lanes of a row
 constexpr int kWarps = 16, kThreads = 32 * kWarps;  // one CTA per SM
-constexpr int kAhead = 4;        // steps of a warp on their way
+constexpr int kMaxStages = 8;
+constexpr int kCtlBytes = 128;
+constexpr long long kAbortDrainNs = 2000000;
 constexpr int kRedPitch = 20;    // floats: the partial sums' stores meet no bank twice
-constexpr size_t kMostSmem = 227 * 1024;
+constexpr int kMostSmem = 227 * 1024;
 constexpr int kXPad = 64;        // bytes behind each token's row: tokens alternate between the banks' halves
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
@@ -117,151 +119,133 @@ __global__ void __launch_bounds__(kSuThreads) decode_su_kernel(const __grid_cons
   }
 }
 
-// What one warp reads per step: 32 codes of row g and of row g + 8 for each lane (g, t), with their (s, b).
-struct Step {
-  uint4 w0, w1;
-  uint32_t s0, s1;
+// How a launch cuts its work.  A tile is MT * 16 rows; `split` warps share a group's tiles, each taking every split-th
+// panel of 256 columns, with `stages` panels of codes on their way or in use.
+struct Cut {
+  int split, groups, stages, tiles;
+  int red_bytes, held_bytes;  // of the warps' sums, the activation
 };
 
-// Loads a step where `ok`.  Elsewhere s = b = 0 make the weights zero whatever the codes' registers hold.
-__device__ __forceinline__ void load_step(Step& s, bool ok, const uint8_t* codes, int codes1, const uint32_t* params,
-                                          int params1) {
-  s.s0 = s.s1 = 0u;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %14, 0;\n\t"
-      "@p ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%10];\n\t"
-      "@p ld.global.nc.L1::no_allocate.v4.u32 {%4, %5, %6, %7}, [%11];\n\t"
-      "@p ld.global.nc.u32 %8, [%12];\n\t"
-      "@p ld.global.nc.u32 %9, [%13];\n\t}"
-      : "=r"(s.w0.x), "=r"(s.w0.y), "=r"(s.w0.z), "=r"(s.w0.w), "=r"(s.w1.x), "=r"(s.w1.y), "=r"(s.w1.z),
-        "=r"(s.w1.w), "+r"(s.s0), "+r"(s.s1)
-      : "l"(codes), "l"(codes + codes1), "l"(params), "l"(params + params1), "r"((uint32_t)ok));
-}
-
-__device__ __forceinline__ uint4 load_shared(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
-  return v;
-}
-
-// `split` warps share a tile of 16 rows: warp i of them has every split-th chunk of the columns from i on, and every
-// split-th 16 of the adapter's, and the warps' sums meet in shared memory (split 1: a warp stores its own).  Tiles go
-// round the SMs first.  A lane's word of 8 codes makes the fragments of two MMAs, whose k index is then a permutation
-// of the columns; the activation's fragments share it: 16 consecutive bytes of token g.  kAhead steps per warp are on
-// their way while one is computed, also across tiles.  The activation stays in shared memory (XS; where its T rows
-// do not fit, its fragments come through L1).
-template <int NT, bool XS>  // NT: tokens / 8
-__global__ void __launch_bounds__(kThreads) decode_kernel(const __grid_constant__ DecodeBatch b, int split) {
-  extern __shared__ __align__(16) uint8_t smem[];
-  float* red = reinterpret_cast<float*>(smem);  // split > 1: [kWarps][NT * 8][kRedPitch]
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int group = warp / split, wg = warp % split;
-  const int slot = group * (int)gridDim.x + (int)blockIdx.x, slots = kWarps / split * (int)gridDim.x;
-  const int T = b.p[0].T, K = b.p[0].K;
-  const __nv_bfloat16* x = b.p[0].x;
+// Each warp keeps a ring of its own filled by tiled copies (a tile's rows and a panel's columns, 128-byte swizzle, zeros
+// outside the matrix), so that no warp waits for another but at the end of a tile that several share.  Tiles go round
+// the SMs first.
+// A lane has the 64 columns of one (s, b) pair of rows g and g + 8: a word of 8 codes makes the fragments of two MMAs,
+// whose k index is then a permutation of the columns; the activation's fragments share it, 16 consecutive bytes of
+// token g.  The warps of a group also share out the adapter's columns by 16, and their sums meet in shared memory
+// (split 1: a warp stores its own).  The activation stays in shared memory (XS; where its T rows do not fit, its
+// fragments come through L1).
+template <int NT, int MT, bool XS>  // NT: tokens / 8; MT: sixteens of rows per tile, which share the activation's fragments
+__global__ void __launch_bounds__(kThreads) decode_kernel(const __grid_constant__ DecodeBatch b,
+                                                          const __grid_constant__ Cut cut) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  constexpr int kChains = NT * MT == 1 ? 2 : 1;  // of dependent MMAs: two at least
+  constexpr int kRows = MT * kTileN;
+  constexpr uint32_t kStageBytes = kRows * (kPanel / 2);
+  const int split = cut.split, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int active = cut.groups * split;
+  const int T = b.p[0].T, K = b.p[0].K, panels = (K + kPanel - 1) / kPanel, pairs = K / 64;
+  uint8_t* red_at = smem + active * cut.stages * kStageBytes;
+  uint8_t* held = red_at + cut.red_bytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(held + cut.held_bytes);
+  int* abort_word = reinterpret_cast<int*>(bars + active * cut.stages);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < active * cut.stages; ++i) mbar_init(smem_u32(bars + i), 1);
+    *abort_word = 0;
+    fence_mbar_init();
+  }
+  __syncthreads();
   if (!b.after_su) griddep_wait();  // otherwise the launch before is this call's, and began after its inputs were there
   griddep_launch_dependents();
-  bool waited = !b.after_su;
+  if (warp >= active) return;
 
-  // the loads' cursor, ahead of the computation's
-  int l_tile = slot, l_proj = 0, l_c = wg;
-  const uint8_t* codes = nullptr;
-  const uint32_t* params = nullptr;
-  int codes1 = 0, params1 = 0;  // from row g to row g + 8 (rows past the last: the last)
-  auto l_open = [&]() {
-    l_c = wg;
-    if (l_tile >= b.tiles) return;
+  const int group = warp / split, wg = warp % split;
+  const int slots = cut.groups * (int)gridDim.x, slot = group * (int)gridDim.x + (int)blockIdx.x;
+  const uint32_t ring_at = warp * cut.stages * kStageBytes;  // from smem
+  const uint32_t ring = smem_u32(smem) + ring_at, bar = smem_u32(bars + warp * cut.stages);
+  const WaitCtl wait{b.status, b.limit_ns};
+  volatile int* abort = abort_word;
+
+  // copies: the cursor of the next one to issue (lane 0)
+  int l_tile = slot, l_proj = 0, l_c = wg, issued = 0;
+  auto issue = [&](int s) {
+    if (l_tile >= cut.tiles) return;
     while (l_proj + 1 < b.n && l_tile >= b.p[l_proj + 1].tile_begin) ++l_proj;
-    const DecodeProj& p = b.p[l_proj];
-    const int n0 = (l_tile - p.tile_begin) * kTileN, r0 = min(n0 + g, p.N - 1), r1 = min(n0 + g + 8, p.N - 1);
-    codes = p.codes + (long long)r0 * (K / 2) + wg * (kChunk / 2) + 16 * t;
-    params = reinterpret_cast<const uint32_t*>(p.params) + (long long)r0 * (K / 64) + wg * (kChunk / 64) + t / 2;
-    codes1 = (r1 - r0) * (K / 2);
-    params1 = (r1 - r0) * (K / 64);
-  };
-  auto fetch = [&](Step& s) {
-    // K is a multiple of 64: the last chunk may be half a one
-    load_step(s, l_tile < b.tiles && l_c * kChunk + 32 * t < K, codes, codes1, params, params1);
+    mbar_arrive_expect_tx(bar + 8 * s, kStageBytes);
+    tma_load_2d(ring + s * kStageBytes, &b.codes[l_proj], bar + 8 * s, l_c * (kPanel / 2),
+                (l_tile - b.p[l_proj].tile_begin) * kRows);
+    ++issued;
     l_c += split;
-    codes += split * (kChunk / 2);
-    params += split * (kChunk / 64);
-    if (l_c * kChunk >= K) {
+    if (l_c >= panels) {
+      l_c = wg;
       l_tile += slots;
-      l_open();
     }
   };
-  l_open();
-  Step steps[kAhead];
-#pragma unroll
-  for (int i = 0; i < kAhead; ++i) fetch(steps[i]);
+  if (lane == 0)
+    for (int s = 0; s < cut.stages; ++s) issue(s);
 
+  // (s, b) pairs, loaded a step ahead: the cursor of the next step's
+  int q_tile = slot, q_proj = 0, q_c = wg;
+  const uint32_t* q_at = nullptr;  // of row g, 8 rows being `pairs` * 8 words
+  int q_rows = 0;                  // rows of the matrix from the tile's first on
+  auto q_open = [&]() {
+    if (q_tile >= cut.tiles) {
+      q_rows = 0;
+      return;
+    }
+    while (q_proj + 1 < b.n && q_tile >= b.p[q_proj + 1].tile_begin) ++q_proj;
+    const DecodeProj& p = b.p[q_proj];
+    const int n0 = (q_tile - p.tile_begin) * kRows;
+    q_rows = p.N - n0;
+    q_at = reinterpret_cast<const uint32_t*>(p.params) + (long long)(n0 + g) * pairs + t;
+  };
+  uint32_t next_pair[2 * MT];
+  auto fetch_pairs = [&]() {
+    const bool in = 4 * q_c + t < pairs;  // the last panel may be a part of one
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i)
+      next_pair[i] = in && g + 8 * i < q_rows ? __ldg(q_at + 4 * q_c + i * 8 * pairs) : 0u;
+    q_c += split;
+    if (q_c >= panels) {
+      q_c = wg;
+      q_tile += slots;
+      q_open();
+    }
+  };
+  q_open();
+  fetch_pairs();
+
+  const __nv_bfloat16* x = b.p[0].x;
   // columns past T are dropped: whatever token their fragments hold
-  uint32_t xs[NT];  // shared address of the lane's fragments of the first chunk
+  uint32_t xs[NT];  // where the lane's fragments of the first panel lie, from smem
   if (XS) {
-    uint8_t* held = smem + (split > 1 ? kWarps * NT * 8 * kRedPitch * 4 : 0);
-    const int units = (K + kChunk - 1) / kChunk * (kChunk / 8), have = K / 8;  // 16 bytes each
-    const int pitch = units * 16 + kXPad;
+    const int units = panels * (kPanel / 8), have = K / 8, x_pitch = units * 16 + kXPad;  // units of 16 bytes of a token
     for (int tok = 0; tok < T; ++tok)
-      for (int v = threadIdx.x; v < units; v += kThreads) {
+      for (int v = threadIdx.x; v < units; v += 32 * active) {
         const uint4 d =
             v < have ? reinterpret_cast<const uint4*>(x + (long long)tok * K)[v] : make_uint4(0u, 0u, 0u, 0u);
-        // unit 4 t + q of a chunk lies at 4 q + t: the lanes of a fragment's load read 64 consecutive bytes a token
-        *reinterpret_cast<uint4*>(held + tok * pitch + ((v & ~15) + 4 * (v & 3) + (v >> 2 & 3)) * 16) = d;
+        // unit 8 t + q of a panel lies at 4 q + t: the lanes of a fragment's load read 64 consecutive bytes a token
+        *reinterpret_cast<uint4*>(held + tok * x_pitch + ((v & ~31) + 4 * (v & 7) + (v >> 3 & 3)) * 16) = d;
       }
 #pragma unroll
-    for (int m = 0; m < NT; ++m) xs[m] = smem_u32(held) + min(g + 8 * m, T - 1) * pitch + 16 * t;
-    __syncthreads();
+    for (int m = 0; m < NT; ++m) xs[m] = (uint32_t)(held - smem) + min(g + 8 * m, T - 1) * x_pitch + 16 * t;
+    __syncwarp();
+    asm volatile("bar.sync 15, %0;" ::"r"(32 * active) : "memory");
   }
-
-  float acc[NT][4];
-  int c = wg;
-  // One step: its products, and the next load into its place; true behind the tile's last.
-  auto step = [&](Step& s) {
-    const uint32_t pa = mul_bf16x2(s.s0, 0x2B806E00u), pb = mul_bf16x2(s.s1, 0x2B806E00u);  // 2^93, 2^-40
-    const uint32_t sa = __byte_perm(pa, 0u, 0x1010), ba = __byte_perm(pa, 0u, 0x3232);
-    const uint32_t sb = __byte_perm(pb, 0u, 0x1010), bb = __byte_perm(pb, 0u, 0x3232);
-    const uint32_t sa4 = mul_bf16x2(sa, 0x3D803D80u), sb4 = mul_bf16x2(sb, 0x3D803D80u);  // 1/16
-    const uint32_t u0[4] = {s.w0.x, s.w0.y, s.w0.z, s.w0.w};
-    const uint32_t u1[4] = {s.w1.x, s.w1.y, s.w1.z, s.w1.w};
-    fetch(s);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      uint4 xv[NT];
-#pragma unroll
-      for (int m = 0; m < NT; ++m) {
-        if (XS)
-          xv[m] = load_shared(xs[m] + c * (kChunk * 2) + 64 * q);
-        else
-          xv[m] = c * kChunk + 32 * t < K
-                      ? __ldg(reinterpret_cast<const uint4*>(x + (long long)min(g + 8 * m, T - 1) * K + c * kChunk +
-                                                             32 * t + 8 * q))
-                      : make_uint4(0u, 0u, 0u, 0u);
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint32_t v0 = h ? u0[q] >> 8 : u0[q], v1 = h ? u1[q] >> 8 : u1[q];
-        const uint32_t a0 = fma_bf16x2(v0 & 0x000F000Fu, sa, ba), a1 = fma_bf16x2(v1 & 0x000F000Fu, sb, bb);
-        const uint32_t a2 = fma_bf16x2(v0 & 0x00F000F0u, sa4, ba), a3 = fma_bf16x2(v1 & 0x00F000F0u, sb4, bb);
-#pragma unroll
-        for (int m = 0; m < NT; ++m)
-          mma_bf16(acc[m], a0, a1, a2, a3, h ? xv[m].z : xv[m].x, h ? xv[m].w : xv[m].y);
-      }
-    }
-    c += split;
-    return c * kChunk >= K;
-  };
-  auto sync_group = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(32 * split) : "memory"); };
-
-  int proj = 0, pos = 0;
-  for (int tile = slot; tile < b.tiles; tile += slots) {
+  // 16-byte units 2 t and 2 t + 1 of a row's 128 bytes, swizzled by the row (its last three bits are g's)
+  const uint32_t even = ring_at + g * (kPanel / 2) + ((2 * t) ^ g) * 16;
+  const uint32_t odd = ring_at + g * (kPanel / 2) + ((2 * t + 1) ^ g) * 16;
+  bool waited = !b.after_su, alive = true;
+  int s = 0, proj = 0;
+  uint32_t phase = 0;
+  for (int tile = slot; tile < cut.tiles; tile += slots) {
     while (proj + 1 < b.n && tile >= b.p[proj + 1].tile_begin) ++proj;
     const DecodeProj& p = b.p[proj];
-    const int n0 = (tile - p.tile_begin) * kTileN, r = p.r;
+    const int n0 = (tile - p.tile_begin) * kRows, r = p.r;
     // the adapter's A operand of 16 columns: rows g and g + 8 of B, columns 2 t (+ 1) and 2 t + 8 (+ 9)
-    auto load_adapter = [&](int j0, uint32_t (&a)[4]) {
+    auto load_adapter = [&](int mt, int j0, uint32_t (&a)[4]) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int n = n0 + g + 8 * (i & 1), j = j0 + 2 * t + 8 * (i >> 1);
+        const int n = n0 + mt * kTileN + g + 8 * (i & 1), j = j0 + 2 * t + 8 * (i >> 1);
         const uint16_t* q = reinterpret_cast<const uint16_t*>(p.B) + (long long)n * r + j;
         a[i] = 0u;
         if (n < p.N && j < r) {
@@ -272,108 +256,211 @@ __global__ void __launch_bounds__(kThreads) decode_kernel(const __grid_constant_
         }
       }
     };
-    uint32_t adapter[4];
-    load_adapter(16 * wg, adapter);
+    uint32_t adapter[MT][4];  // its first columns, on their way meanwhile
 #pragma unroll
-    for (int m = 0; m < NT; ++m)
+    for (int mt = 0; mt < MT; ++mt) load_adapter(mt, 16 * wg, adapter[mt]);
+    float acc[kChains][MT][NT][4] = {};
+    for (int c = wg; c < panels; c += split) {
+      uint32_t sc[MT][2], sc4[MT][2], of[MT][2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[m][e] = 0.f;
-    c = wg;
-    for (bool done = false; !done;) {
-      switch (pos) {
-        case 0:
-          pos = 1;
-          if ((done = step(steps[0]))) break;
-          [[fallthrough]];
-        case 1:
-          pos = 2;
-          if ((done = step(steps[1]))) break;
-          [[fallthrough]];
-        case 2:
-          pos = 3;
-          if ((done = step(steps[2]))) break;
-          [[fallthrough]];
-        default:
-          pos = 0;
-          done = step(steps[3]);
+      for (int i = 0; i < 2 * MT; ++i) {  // eights of rows
+        const uint32_t sb = mul_bf16x2(next_pair[i], 0x2B806E00u);  // 2^93, 2^-40
+        sc[i / 2][i % 2] = __byte_perm(sb, 0u, 0x1010);
+        of[i / 2][i % 2] = __byte_perm(sb, 0u, 0x3232);
+        sc4[i / 2][i % 2] = mul_bf16x2(sc[i / 2][i % 2], 0x3D803D80u);  // 1/16
       }
+      fetch_pairs();
+      if (alive) alive = mbar_wait(bar + 8 * s, phase, wait, abort);
+      __syncwarp();  // the MMAs need the warp whole
+      const uint32_t at = s * kStageBytes, xc = c * (kPanel * 2);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {  // a lane's first 32 columns and its last
+        uint4 w[MT][2];
+#pragma unroll
+        for (int i = 0; i < 2 * MT; ++i)
+          w[i / 2][i % 2] = *reinterpret_cast<const uint4*>(smem + at + (half ? odd : even) + i * 8 * (kPanel / 2));
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint4 xv[NT];
+#pragma unroll
+          for (int m = 0; m < NT; ++m) {
+            if (XS)
+              xv[m] = *reinterpret_cast<const uint4*>(smem + xs[m] + xc + 256 * half + 64 * q);
+            else
+              xv[m] = 4 * c + t < pairs ? __ldg(reinterpret_cast<const uint4*>(
+                                              x + (long long)min(g + 8 * m, T - 1) * K + c * kPanel + 64 * t + 32 * half +
+                                              8 * q))
+                                        : make_uint4(0u, 0u, 0u, 0u);
+          }
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            const uint4 w0 = w[mt][0], w1 = w[mt][1];
+            const uint32_t u0 = q == 0 ? w0.x : q == 1 ? w0.y : q == 2 ? w0.z : w0.w;
+            const uint32_t u1 = q == 0 ? w1.x : q == 1 ? w1.y : q == 2 ? w1.z : w1.w;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t v0 = h ? u0 >> 8 : u0, v1 = h ? u1 >> 8 : u1;
+              const uint32_t a0 = fma_bf16x2(v0 & 0x000F000Fu, sc[mt][0], of[mt][0]);
+              const uint32_t a1 = fma_bf16x2(v1 & 0x000F000Fu, sc[mt][1], of[mt][1]);
+              const uint32_t a2 = fma_bf16x2(v0 & 0x00F000F0u, sc4[mt][0], of[mt][0]);
+              const uint32_t a3 = fma_bf16x2(v1 & 0x00F000F0u, sc4[mt][1], of[mt][1]);
+#pragma unroll
+              for (int m = 0; m < NT; ++m)
+                mma_bf16(acc[h % kChains][mt][m], a0, a1, a2, a3, h ? xv[m].z : xv[m].x, h ? xv[m].w : xv[m].y);
+            }
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0 && alive) issue(s);
+      if (++s == cut.stages) {
+        s = 0;
+        phase ^= 1u;
+      }
+    }
+    if (kChains == 2) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[0][0][0][e] += acc[kChains - 1][0][0][e];
     }
     for (int j0 = 16 * wg; j0 < r; j0 += 16 * split) {
       if (!waited) {
         griddep_wait();  // su
         waited = true;
       }
-      if (j0 != 16 * wg) load_adapter(j0, adapter);
+      uint4 lo[NT], hi[NT];
 #pragma unroll
       for (int m = 0; m < NT; ++m) {
         const uint4* su =
             reinterpret_cast<const uint4*>(p.su + (min(g + 8 * m, T - 1) * su_steps(r) + j0 / 16) * kSuWords + 8 * t);
-        const uint4 lo = su[0], hi = su[1];
-        mma_bf16(acc[m], adapter[0], adapter[1], adapter[2], adapter[3], lo.x, hi.x);
-        mma_bf16(acc[m], adapter[0], adapter[1], adapter[2], adapter[3], lo.y, hi.y);
-        mma_bf16(acc[m], adapter[0], adapter[1], adapter[2], adapter[3], lo.z, hi.z);
+        lo[m] = su[0];
+        hi[m] = su[1];
+      }
+      __syncwarp();
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        if (j0 != 16 * wg) load_adapter(mt, j0, adapter[mt]);
+        __syncwarp();
+        const uint32_t(&a)[4] = adapter[mt];
+#pragma unroll
+        for (int m = 0; m < NT; ++m) {
+          mma_bf16(acc[0][mt][m], a[0], a[1], a[2], a[3], lo[m].x, hi[m].x);
+          mma_bf16(acc[0][mt][m], a[0], a[1], a[2], a[3], lo[m].y, hi[m].y);
+          mma_bf16(acc[0][mt][m], a[0], a[1], a[2], a[3], lo[m].z, hi[m].z);
+        }
       }
     }
-    if (split == 1) {
+    auto sync_group = [&]() {
+      __syncwarp();  // a warp in parts would count as several
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(32 * split) : "memory");
+    };
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      if (split == 1) {
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int tok = 8 * m + 2 * t + (e & 1), n = n0 + mt * kTileN + g + 8 * (e >> 1);
+            if (tok < T && n < p.N) p.y[(long long)tok * p.N + n] = __float2bfloat16(acc[0][mt][m][e] * 0x1p40f);
+          }
+        continue;
+      }
+      float* red = reinterpret_cast<float*>(red_at);  // [active][NT * 8][kRedPitch]
+      float* mine = red + warp * (NT * 8 * kRedPitch);
+      sync_group();  // the sums of the tile before are read
 #pragma unroll
       for (int m = 0; m < NT; ++m)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int tok = 8 * m + 2 * t + (e & 1), n = n0 + g + 8 * (e >> 1);
-          if (tok < T && n < p.N) p.y[(long long)tok * p.N + n] = __float2bfloat16(acc[m][e] * 0x1p40f);
-        }
-      continue;
-    }
-    sync_group();  // the sums of the tile before are read
-    float* mine = red + warp * (NT * 8 * kRedPitch);
-#pragma unroll
-    for (int m = 0; m < NT; ++m)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) mine[(8 * m + 2 * t + (e & 1)) * kRedPitch + g + 8 * (e >> 1)] = acc[m][e];
-    sync_group();
-    const float* sums = red + group * split * (NT * 8 * kRedPitch);
-    for (int o = wg * 32 + lane; o < kTileN * T; o += 32 * split) {
-      const int tok = o / kTileN, row = o % kTileN, n = n0 + row;
-      float v = 0.f;
+        for (int e = 0; e < 4; ++e) mine[(8 * m + 2 * t + (e & 1)) * kRedPitch + g + 8 * (e >> 1)] = acc[0][mt][m][e];
+      sync_group();
+      const float* sums = red + group * split * (NT * 8 * kRedPitch);
+      for (int o = wg * 32 + lane; o < kTileN * T; o += 32 * split) {
+        const int tok = o / kTileN, row = o % kTileN, n = n0 + mt * kTileN + row;
+        float v = 0.f;
 #pragma unroll 4
-      for (int w = 0; w < split; ++w) v += sums[(w * NT * 8 + tok) * kRedPitch + row];
-      if (n < p.N) p.y[(long long)tok * p.N + n] = __float2bfloat16(v * 0x1p40f);
+        for (int w = 0; w < split; ++w) v += sums[(w * NT * 8 + tok) * kRedPitch + row];
+        if (n < p.N) p.y[(long long)tok * p.N + n] = __float2bfloat16(v * 0x1p40f);
+      }
     }
   }
   if (!waited) griddep_wait();  // no grid ends before the ones it follows
+  // a wait gave up: the warp's copies still in flight land before the shared memory is released (bounded)
+  if (!alive && lane == 0)
+    for (int i = issued - 1; i >= 0 && i >= issued - cut.stages; --i)
+      mbar_wait_drain(bar + 8 * (i % cut.stages), (uint32_t)((i / cut.stages) & 1), kAbortDrainNs);
 }
 
-// Warps per tile.  More of them finish a tile sooner, fewer share less: the cost of a choice is the rounds of the
-// SMs' slots, times the chunks of a warp and what its end takes, in chunks.
-int choose_split(int tiles, int chunks, int num_sms) {
-  int best = 1;
-  double least = 0.0;
-  for (int split = 1; split <= kWarps && split <= chunks; split *= 2) {
-    const int slots = num_sms * (kWarps / split);
-    const double cost = (double)((tiles + slots - 1) / slots) * ((chunks + split - 1) / split + (split == 1 ? 0.5 : 1.5));
-    if (split == 1 || cost < least) {
-      best = split;
-      least = cost;
+int tiles_of(const DecodeProj& p, int mt) { return (p.N + mt * kTileN - 1) / (mt * kTileN); }
+int panels_of(const DecodeProj& p) { return (p.K + kPanel - 1) / kPanel; }
+
+// The cheapest cut, in clocks of an SM: the instructions of its tiles at the rate that its warps reach, or the longest
+// warp's path, whichever takes longer.
+bool choose_cut(const DecodeBatch& b, int nt, int mt, bool xs, int num_sms, Cut* best, double* least) {
+  const DecodeProj& p = b.p[0];
+  const int panels = panels_of(p);
+  int tiles = 0;
+  for (int i = 0; i < b.n; ++i) tiles += tiles_of(b.p[i], mt);
+  const int per_sm = (tiles + num_sms - 1) / num_sms;
+  bool found = false;
+  for (int split : {1, 2, 3, 4, 6, 8, 12, 16}) {
+    if (split > panels) break;
+    int last = 0;
+    for (int rounds = (per_sm * split + kWarps - 1) / kWarps; rounds <= per_sm; ++rounds) {
+      Cut c;
+      c.split = split;
+      c.tiles = tiles;
+      c.groups = (per_sm + rounds - 1) / rounds;
+      if (c.groups == last) continue;
+      last = c.groups;
+      const int active = c.groups * split;
+      if (active < 8 && rounds > 1) break;
+      c.red_bytes = split > 1 ? active * nt * 8 * kRedPitch * 4 : 0;
+      c.held_bytes = xs ? (p.T * (panels * (kPanel * 2) + kXPad) + 127) & ~127 : 0;
+      const int room = kMostSmem - kCtlBytes - c.red_bytes - c.held_bytes;
+      c.stages = std::min(std::min(kMaxStages, (panels + split - 1) / split * rounds),
+                          room / (active * (mt * kTileN * (kPanel / 2) + 8)));
+      if (c.stages < std::min(2, (panels + split - 1) / split * rounds)) continue;
+      const double rate = std::min(2.7, (mt == 1 ? 0.17 : 0.2) * active);
+      const double step = (nt == 1 ? 205 : mt == 1 ? 240 : 220) * mt;
+      const double work = per_sm * (panels * step + (split > 1 ? 100.0 * split : 60.0) * mt) / rate;
+      const double path = (double)rounds * ((panels + split - 1) / split) * mt * 500;
+      const double cost = std::max(work, path) + rounds * (split > 1 ? 300.0 : 100.0);
+      if (cost < *least) {
+        *least = cost;
+        *best = c;
+        found = true;
+      }
     }
   }
-  return best;
+  return found;
 }
 
-template <int NT, bool XS>
-cudaError_t launch_main(const DecodeBatch& b, int split, size_t smem, int num_sms, cudaStream_t st) {
+template <int NT, int MT, bool XS>
+cudaError_t launch_main(DecodeBatch& b, const Cut& cut, int num_sms, cudaStream_t st) {
   static std::atomic<unsigned long long> done{0};
-  const cudaError_t e = set_smem_once(decode_kernel<NT, XS>, kMostSmem, done);
+  const cudaError_t e = set_smem_once(decode_kernel<NT, MT, XS>, kMostSmem, done);
   if (e != cudaSuccess) return e;
-  return launch_kernel(decode_kernel<NT, XS>, dim3(std::min(b.tiles, num_sms)), dim3(kThreads), smem, st, 1, b, split);
+  int begin = 0;
+  for (int i = 0; i < b.n; ++i) {
+    DecodeProj& p = b.p[i];
+    p.tile_begin = begin;
+    begin += tiles_of(p, MT);
+    if (!make_codes_map(&b.codes[i], p.codes, p.K / 2, p.N, kPanel / 2, MT * kTileN)) return cudaErrorInvalidValue;
+  }
+  const int active = cut.groups * cut.split;
+  const size_t smem = (size_t)active * cut.stages * (MT * kTileN * (kPanel / 2) + 8) + cut.red_bytes + cut.held_bytes + kCtlBytes;
+  return launch_kernel(decode_kernel<NT, MT, XS>, dim3(std::min(cut.tiles, num_sms)), dim3(kThreads), smem, st, 1, b, cut);
 }
 
 template <int NT>
-cudaError_t launch_main(const DecodeBatch& b, int num_sms, cudaStream_t st) {
-  const int chunks = (b.p[0].K + kChunk - 1) / kChunk, split = choose_split(b.tiles, chunks, num_sms);
-  const size_t red = split > 1 ? (size_t)kWarps * NT * 8 * kRedPitch * 4 : 0;
-  const size_t held = (size_t)b.p[0].T * (chunks * (kChunk * 2) + kXPad);
-  return red + held <= kMostSmem ? launch_main<NT, true>(b, split, red + held, num_sms, st)
-                                 : launch_main<NT, false>(b, split, red, num_sms, st);
+cudaError_t launch_main(DecodeBatch& b, int num_sms, cudaStream_t st) {
+  Cut cut;
+  double least = 1e300;
+  const bool one = choose_cut(b, NT, 1, true, num_sms, &cut, &least);
+  if (choose_cut(b, NT, 2, true, num_sms, &cut, &least)) return launch_main<NT, 2, true>(b, cut, num_sms, st);
+  if (one) return launch_main<NT, 1, true>(b, cut, num_sms, st);
+  if (!choose_cut(b, NT, 1, false, num_sms, &cut, &least)) return cudaErrorInvalidConfiguration;
+  return launch_main<NT, 1, false>(b, cut, num_sms, st);
 }
 
 cudaError_t launch_su(const DecodeBatch& b, int most, cudaStream_t st) {
@@ -406,15 +493,14 @@ cudaError_t launch_decode(DecodeBatch& b, int num_sms, cudaStream_t st) {
   for (int i = 0; i < b.n; ++i) {
     if (taken[i]) continue;
     DecodeBatch same;
-    same.n = same.tiles = 0;
+    same.n = 0;
     same.after_su = b.rows > 0;
+    same.status = b.status;
+    same.limit_ns = b.limit_ns;
     for (int j = i; j < b.n; ++j) {
       if (taken[j] || b.p[j].x != b.p[i].x || b.p[j].T != b.p[i].T || b.p[j].K != b.p[i].K) continue;
       taken[j] = true;
-      DecodeProj& p = same.p[same.n++];
-      p = b.p[j];
-      p.tile_begin = same.tiles;
-      same.tiles += (p.N + kTileN - 1) / kTileN;
+      same.p[same.n++] = b.p[j];
     }
     const cudaError_t e = b.p[i].T <= 8 ? launch_main<1>(same, num_sms, st) : launch_main<2>(same, num_sms, st);
     if (e != cudaSuccess) return e;

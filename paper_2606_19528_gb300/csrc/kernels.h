@@ -411,12 +411,17 @@ struct DecodeProj {
 };
 
 struct DecodeBatch {
+  CUtensorMap codes[kDecodeMaxProjs];
   DecodeProj p[kDecodeMaxProjs];
-  int n, tiles, rows;
+  int n, rows;
   int after_su;  // the launch follows one that computes su
+  int* status;
+  long long limit_ns;
 };
 
 size_t decode_su_bytes(int64_t T, int64_t r);
+// Tensor map of a matrix of bytes [rows, width] for boxes of box_width (128) x box_rows, 128-byte swizzle, zeros outside.
+bool make_codes_map(CUtensorMap* m, const void* ptr, int width, int rows, int box_width, int box_rows);
 // su of every projection with an adapter (nothing to launch without one), then y = x W^T + su B^T.  The caller
 // sets all but the begins and the totals.
 cudaError_t launch_decode(DecodeBatch& b, int num_sms, cudaStream_t stream);

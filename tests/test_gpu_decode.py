@@ -177,6 +177,36 @@ def test_same_bits_every_time_and_on_another_stream():
         assert all(torch.equal(p.y, f) for p, f in zip(ps, first))
 
 
+@pytest.mark.parametrize("T,K,N", [(16, 3072, 30000), (16, 1024, 20001), (8, 3072, 30000), (9, 320, 50000),
+                                   (16, 6144, 6000), (3, 11008, 2048), (16, 12288, 1000)])
+def test_many_tiles_come_out_the_same_in_every_call(T, K, N):
+    """Every SM takes many tiles through its rings, with little room for them beside 16 tokens: 100 calls, bit for
+    bit, and against the product in fp32."""
+    g = torch.Generator(device="cuda").manual_seed(K + N)
+    codes = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+    sd = K ** -0.5
+    s = torch.empty(N, K // 64, device="cuda").uniform_(0.2, 0.45, generator=g) * sd
+    params = torch.stack([s, -7.5 * s], dim=-1).to(torch.bfloat16).contiguous()
+    x = torch.randn(T, K, generator=g, device="cuda").to(torch.bfloat16)
+    words = codes.view(torch.int32)[:, :, None, None]
+    shift = torch.tensor([[0, 16], [4, 20], [8, 24], [12, 28]], device="cuda", dtype=torch.int32)
+    q = ((words >> shift) & 15).float().view(N, K // 64, 64)
+    W = (params[:, :, :1].float() * q + params[:, :, 1:].float()).to(torch.bfloat16).float().view(N, K)
+    y = torch.full((T, N), float("nan"), dtype=torch.bfloat16, device="cuda")
+    projs = lora.make_projs([lora.make_proj(lora.make_shape(T, K, N, 0, 1.0), x=x, y=y,
+                                            Wq=lora.make_q4(codes, params))])
+    lora.lora_decode_q4(projs, None, 0)
+    first, bad = y.clone(), 0
+    for _ in range(100):
+        y.zero_()
+        lora.lora_decode_q4(projs, None, 0)
+        bad += (y != first).sum()
+    assert int(bad) == 0
+    want = x.float() @ W.T
+    size = x.float().abs() @ W.abs().T  # the bound of the module's head, twice the sums' part for the fp32 product
+    assert ((first.float() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -19 * size).all()
+
+
 def test_chain_of_calls_in_a_graph():
     """y of one call is x of the next, captured and replayed with other inputs in place."""
     K = 256
