@@ -2228,9 +2228,14 @@ int clip_check_ptrs(const lora_grad* grads, int n) {
 
 void note_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
 
-bool make_codes_map(CUtensorMap* m, const void* ptr, int width, int rows, int box_width, int box_rows) {
+bool make_bytes_map(CUtensorMap* m, const void* ptr, int width, int rows, int box_width, int box_rows) {
   return make_map_plain(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, ptr, (uint64_t)width, (uint64_t)rows, (uint64_t)width,
                         (uint32_t)box_width, (uint32_t)box_rows, CU_TENSOR_MAP_SWIZZLE_128B) == LORA_OK;
+}
+
+bool make_bf16_map(CUtensorMap* m, const void* ptr, int width, int rows, int box_width, int box_rows) {
+  return make_map(m, ptr, (uint64_t)width, (uint64_t)rows, (uint64_t)width, (uint32_t)box_width, (uint32_t)box_rows) ==
+         LORA_OK;
 }
 
 // Code the calling thread's most recent entry point returned (lora_last_error).
@@ -2711,12 +2716,12 @@ int lora_decode_q4(const lora_proj* projs, int n_proj, void* workspace, size_t w
     p.A = cb(q.A);
     p.B = cb(q.B);
     p.y = mb(q.y);
-    p.su = at<uint32_t>(workspace, off);
     p.scale = q.shape.scale;
     p.T = (int)q.shape.T;
     p.N = (int)q.shape.d_out;
     p.K = (int)q.shape.d_in;
     p.r = (int)q.shape.rank;
+    set_decode_su(p, at<uint8_t>(workspace, off));
     off += up256(decode_su_bytes(p.T, p.r));
   }
   return rec(launch_decode(b, d->num_sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LORA_OK : LORA_ECUDA);

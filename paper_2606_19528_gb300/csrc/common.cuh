@@ -394,6 +394,29 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return *reinterpret_cast<uint32_t*>(&h);
 }
 
+// Dequantization scaled by 2^-40, in one FMA per pair of codes.  A bf16 whose exponent field is 0 or 1 is its low 8
+// bits as an integer, times 2^-133: the codes in bits 0..3 and 16..19 of a word are a pair of bf16 q * 2^-133 as they
+// lie, those in bits 4..7 and 20..23 a pair 16 q * 2^-133.  One FMA with s * 2^93 (s * 2^89 for the latter) and
+// b * 2^-40 gives 2^-40 (s q + b), rounded once like dq_pair's s q + b.  (Valid for |s| < 2^35; a weight below 2^-86
+// loses bits.)
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+// (s, b) -> (s * 2^93, b * 2^-40); the former twice -> s * 2^89 twice
+__device__ __forceinline__ uint32_t dq40_pair(uint32_t sb) { return fma_bf16x2(sb, 0x2B806E00u, 0x80008000u); }
+__device__ __forceinline__ uint32_t dq40_high(uint32_t s2) { return fma_bf16x2(s2, 0x3D803D80u, 0x80008000u); }
+// The eight codes of a word, in the order of the columns: s0 = s * 2^93 twice, s1 = s * 2^89 twice, b2 = b * 2^-40 twice.
+__device__ __forceinline__ void dq40_word(uint32_t w, uint32_t s0, uint32_t s1, uint32_t b2, uint32_t& o0, uint32_t& o1,
+                                          uint32_t& o2, uint32_t& o3) {
+  const uint32_t v = w >> 8;
+  o0 = fma_bf16x2(w & 0x000F000Fu, s0, b2);
+  o1 = fma_bf16x2(w & 0x00F000F0u, s1, b2);
+  o2 = fma_bf16x2(v & 0x000F000Fu, s0, b2);
+  o3 = fma_bf16x2(v & 0x00F000F0u, s1, b2);
+}
+
 // Two 4-bit codes -> bf16x2 (s * q + b): the codes sit at bits 0..3 and
 // 16..19 of `w`; OR-ing in the exponent of 128 gives exactly 128 + q per half,
 // the first FMA takes 128 off (exact), the second rounds s * q + b once.

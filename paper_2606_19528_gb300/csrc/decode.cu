@@ -8,11 +8,7 @@
 // weights more, and the tcgen05 path wants its operands in shared memory, where the round trip of the dequantized
 // weights alone costs more than the products of 16 tokens.
 //
-// Dequantizing takes 9 instructions per 8 codes.  A bf16 whose exponent field is 0 or 1 is its low 8 bits as an
-// integer, times 2^-133: the codes in bits 0..3 and 16..19 of a word are a pair of bf16 q * 2^-133 as they lie, those
-// in bits 4..7 and 20..23 a pair 16 q * 2^-133.  One FMA with s * 2^93 (or s * 2^89) and b * 2^-40 then gives
-// 2^-40 (s q + b), rounded to bf16 once like the training kernels' weight, and the sums are scaled back by 2^40.
-// (Valid for |s| < 2^35; a weight below 2^-86 loses bits.)
+// Dequantizing takes 9 instructions per 8 codes (dq40_word); the sums are scaled back by 2^40.
 //
 // su enters the same MMAs as three bf16 terms, which hold all 24 bits of its fp32 value.
 #include <algorithm>
@@ -24,14 +20,9 @@ namespace lora {
 namespace {
 
 constexpr int kTileN = 16;       // output rows of a tile: M of the MMA
-constexpr int kPanel = 256;      // columns of a warp's step: a 64-wide group to each of the four lanes of a row
-constexpr int kWarps = 16, kThreads = 32 * kWarps;  // one CTA per SM
-constexpr int kMaxStages = 8;
-constexpr int kCtlBytes = 128;
-constexpr long long kAbortDrainNs = 2000000;
+constexpr int kChunk = 128;      // columns of a warp's step: two 64-wide groups, 32 columns a lane
+constexpr int kMostThreads = 512;
 constexpr int kRedPitch = 20;    // floats: the partial sums' stores meet no bank twice
-constexpr int kMostSmem = 227 * 1024;
-constexpr int kXPad = 64;        // bytes behind each token's row: tokens alternate between the banks' halves
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                          uint32_t b0, uint32_t b1) {
@@ -41,25 +32,24 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c) {
-  uint32_t d;
-  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
+__device__ __forceinline__ uint4 load_codes(const uint8_t* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
+  return v;
 }
-
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) { return fma_bf16x2(a, b, 0x80008000u); }
 
 __device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// su as the MMAs' B operand reads it, for 16 adapter columns at a time: [T][su_steps(r)][t][8 words], where lane t's
-// words 0..2 hold columns 2 t and 2 t + 1 in three terms, and words 4..6 columns 2 t + 8 and 2 t + 9.  Times 2^-40 like
-// the weights, zeros behind column r.
-constexpr int kSuTerms = 3, kSuWords = 32;
-__host__ __device__ constexpr int su_steps(int r) { return (r + 15) / 16; }
-__device__ __forceinline__ int su_at(int r, int tok, int col, int term) {  // in 16-bit units
+// Where column `col` of token `tok` lies, in 16-bit units.
+__device__ __forceinline__ int su_at(int r, int tok, int col, int term) {
   const int c = col & 15;
   return 2 * ((tok * su_steps(r) + col / 16) * kSuWords + (c & 7) / 2 * 8 + c / 8 * 4 + term) + (c & 1);
+}
+__device__ __forceinline__ int su_image_at(int r, int tok, int col, int term) {
+  return (term * su_blocks(r) + col / 64) * (kSuBlock / 2) + tok * 64 + ((col % 64 / 8) ^ (tok & 7)) * 8 + col % 8;
 }
 
 // One block per (projection, adapter row j): su[t, j] = scale * x_t . A_j for up to TT tokens.
@@ -106,361 +96,160 @@ __global__ void __launch_bounds__(kSuThreads) decode_su_kernel(const __grid_cons
 #pragma unroll
     for (int w = 0; w < kSuThreads / 32; ++w) v += part[w][threadIdx.x];
     v *= p.scale * 0x1p-40f;
-    __nv_bfloat16* su = reinterpret_cast<__nv_bfloat16*>(p.su);
+    __nv_bfloat16 *su = reinterpret_cast<__nv_bfloat16*>(p.su), *image = reinterpret_cast<__nv_bfloat16*>(p.su_image);
+    auto put = [&](int col, int e, __nv_bfloat16 term) {
+      su[su_at(p.r, threadIdx.x, col, e)] = term;
+      image[su_image_at(p.r, threadIdx.x, col, e)] = term;
+    };
 #pragma unroll
     for (int e = 0; e < kSuTerms; ++e) {
       const __nv_bfloat16 term = __float2bfloat16(v);
-      su[su_at(p.r, threadIdx.x, j, e)] = term;
+      put(j, e, term);
       v = isfinite(v) ? v - __bfloat162float(term) : 0.f;
     }
     if (j == p.r - 1)
       for (int col = p.r; col < 16 * su_steps(p.r); ++col)
-        for (int e = 0; e < kSuTerms; ++e) su[su_at(p.r, threadIdx.x, col, e)] = __float2bfloat16(0.f);
+        for (int e = 0; e < kSuTerms; ++e) put(col, e, __float2bfloat16(0.f));
   }
 }
 
-// How a launch cuts its work.  A tile is MT * 16 rows; `split` warps share a group's tiles, each taking every split-th
-// panel of 256 columns, with `stages` panels of codes on their way or in use.
-struct Cut {
-  int split, groups, stages, tiles;
-  int red_bytes, held_bytes;  // of the warps' sums, the activation
+// What a warp reads per step of 128 columns: 32 codes of row g and of row g + 8 for each lane (g, t), with their (s, b).
+struct Step {
+  uint4 w0, w1;
+  uint32_t s0, s1;
 };
 
-// Each warp keeps a ring of its own filled by tiled copies (a tile's rows and a panel's columns, 128-byte swizzle, zeros
-// outside the matrix), so that no warp waits for another but at the end of a tile that several share.  Tiles go round
-// the SMs first.
-// A lane has the 64 columns of one (s, b) pair of rows g and g + 8: a word of 8 codes makes the fragments of two MMAs,
-// whose k index is then a permutation of the columns; the activation's fragments share it, 16 consecutive bytes of
-// token g.  The warps of a group also share out the adapter's columns by 16, and their sums meet in shared memory
-// (split 1: a warp stores its own).  The activation stays in shared memory (XS; where its T rows do not fit, its
-// fragments come through L1).
-template <int NT, int MT, bool XS>  // NT: tokens / 8; MT: sixteens of rows per tile, which share the activation's fragments
-__global__ void __launch_bounds__(kThreads) decode_kernel(const __grid_constant__ DecodeBatch b,
-                                                          const __grid_constant__ Cut cut) {
-  extern __shared__ __align__(1024) uint8_t smem[];
-  constexpr int kChains = NT * MT == 1 ? 2 : 1;  // of dependent MMAs: two at least
-  constexpr int kRows = MT * kTileN;
-  constexpr uint32_t kStageBytes = kRows * (kPanel / 2);
-  const int split = cut.split, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int active = cut.groups * split;
-  const int T = b.p[0].T, K = b.p[0].K, panels = (K + kPanel - 1) / kPanel, pairs = K / 64;
-  uint8_t* red_at = smem + active * cut.stages * kStageBytes;
-  uint8_t* held = red_at + cut.red_bytes;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(held + cut.held_bytes);
-  int* abort_word = reinterpret_cast<int*>(bars + active * cut.stages);
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < active * cut.stages; ++i) mbar_init(smem_u32(bars + i), 1);
-    *abort_word = 0;
-    fence_mbar_init();
-  }
-  __syncthreads();
+// One block per 16 output rows, its warps sharing out the columns: warp i has every warps-th chunk of 128 from i on, and
+// every warps-th 16 of the adapter's columns.  A step's weights are loaded while the one before is computed; loading
+// two to four steps ahead takes the registers of as many warps and is slower.  A lane's word of 8 codes makes the fragments of two MMAs, whose k index is
+// then a permutation of the columns; the activation's fragments share it: 16 consecutive bytes of token g, which come
+// through L1.
+template <int NT>  // tokens / 8
+__global__ void __launch_bounds__(kMostThreads) decode_kernel(const __grid_constant__ DecodeBatch b) {
+  constexpr int kChains = NT == 1 ? 2 : 1;  // of dependent MMAs: two at least
+  const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   if (!b.after_su) griddep_wait();  // otherwise the launch before is this call's, and began after its inputs were there
   griddep_launch_dependents();
-  if (warp >= active) return;
-
-  const int group = warp / split, wg = warp % split;
-  const int slots = cut.groups * (int)gridDim.x, slot = group * (int)gridDim.x + (int)blockIdx.x;
-  const uint32_t ring_at = warp * cut.stages * kStageBytes;  // from smem
-  const uint32_t ring = smem_u32(smem) + ring_at, bar = smem_u32(bars + warp * cut.stages);
-  const WaitCtl wait{b.status, b.limit_ns};
-  volatile int* abort = abort_word;
-
-  // copies: the cursor of the next one to issue (lane 0)
-  int l_tile = slot, l_proj = 0, l_c = wg, issued = 0;
-  auto issue = [&](int s) {
-    if (l_tile >= cut.tiles) return;
-    while (l_proj + 1 < b.n && l_tile >= b.p[l_proj + 1].tile_begin) ++l_proj;
-    mbar_arrive_expect_tx(bar + 8 * s, kStageBytes);
-    tma_load_2d(ring + s * kStageBytes, &b.codes[l_proj], bar + 8 * s, l_c * (kPanel / 2),
-                (l_tile - b.p[l_proj].tile_begin) * kRows);
-    ++issued;
-    l_c += split;
-    if (l_c >= panels) {
-      l_c = wg;
-      l_tile += slots;
+  int i = 0;
+  while (i + 1 < b.n && (int)blockIdx.x >= b.p[i + 1].tile_begin) ++i;
+  const DecodeProj& p = b.p[i];
+  const int n0 = ((int)blockIdx.x - p.tile_begin) * kTileN, K = p.K, T = p.T, r = p.r;
+  const long long r0 = min(n0 + g, p.N - 1), r1 = min(n0 + g + 8, p.N - 1);
+  const uint8_t *c0 = p.codes + r0 * (K / 2) + 16 * t, *c1 = p.codes + r1 * (K / 2) + 16 * t;
+  const uint32_t* q0 = reinterpret_cast<const uint32_t*>(p.params) + r0 * (K / 64) + t / 2;
+  const uint32_t* q1 = reinterpret_cast<const uint32_t*>(p.params) + r1 * (K / 64) + t / 2;
+  // K is a multiple of 64: the last chunk may be half a one, where s = b = 0 make the weights zero
+  auto fetch = [&](Step& s, int c) {
+    s.s0 = s.s1 = 0u;
+    s.w0 = s.w1 = make_uint4(0u, 0u, 0u, 0u);
+    if (c * kChunk + 32 * t < K) {
+      s.w0 = load_codes(c0 + c * (kChunk / 2));
+      s.w1 = load_codes(c1 + c * (kChunk / 2));
+      s.s0 = __ldg(q0 + 2 * c);
+      s.s1 = __ldg(q1 + 2 * c);
     }
   };
-  if (lane == 0)
-    for (int s = 0; s < cut.stages; ++s) issue(s);
+  Step s;
+  fetch(s, warp);
 
-  // (s, b) pairs, loaded a step ahead: the cursor of the next step's
-  int q_tile = slot, q_proj = 0, q_c = wg;
-  const uint32_t* q_at = nullptr;  // of row g, 8 rows being `pairs` * 8 words
-  int q_rows = 0;                  // rows of the matrix from the tile's first on
-  auto q_open = [&]() {
-    if (q_tile >= cut.tiles) {
-      q_rows = 0;
-      return;
-    }
-    while (q_proj + 1 < b.n && q_tile >= b.p[q_proj + 1].tile_begin) ++q_proj;
-    const DecodeProj& p = b.p[q_proj];
-    const int n0 = (q_tile - p.tile_begin) * kRows;
-    q_rows = p.N - n0;
-    q_at = reinterpret_cast<const uint32_t*>(p.params) + (long long)(n0 + g) * pairs + t;
-  };
-  uint32_t next_pair[2 * MT];
-  auto fetch_pairs = [&]() {
-    const bool in = 4 * q_c + t < pairs;  // the last panel may be a part of one
+  // the adapter's A operand of 16 columns: rows g and g + 8 of B, columns 2 t (+ 1) and 2 t + 8 (+ 9)
+  auto load_adapter = [&](int j0, uint32_t (&a)[4]) {
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i)
-      next_pair[i] = in && g + 8 * i < q_rows ? __ldg(q_at + 4 * q_c + i * 8 * pairs) : 0u;
-    q_c += split;
-    if (q_c >= panels) {
-      q_c = wg;
-      q_tile += slots;
-      q_open();
+    for (int e = 0; e < 4; ++e) {
+      const int n = n0 + g + 8 * (e & 1), j = j0 + 2 * t + 8 * (e >> 1);
+      const uint16_t* q = reinterpret_cast<const uint16_t*>(p.B) + (long long)n * r + j;
+      a[e] = 0u;
+      if (n < p.N && j < r) {
+        if (r % 2 == 0)
+          a[e] = __ldg(reinterpret_cast<const uint32_t*>(q));
+        else
+          a[e] = __ldg(q) | (j + 1 < r ? (uint32_t)__ldg(q + 1) << 16 : 0u);
+      }
     }
   };
-  q_open();
-  fetch_pairs();
+  uint32_t adapter[4];
+  load_adapter(16 * warp, adapter);
 
-  const __nv_bfloat16* x = b.p[0].x;
-  // columns past T are dropped: whatever token their fragments hold
-  uint32_t xs[NT];  // where the lane's fragments of the first panel lie, from smem
-  if (XS) {
-    const int units = panels * (kPanel / 8), have = K / 8, x_pitch = units * 16 + kXPad;  // units of 16 bytes of a token
-    for (int tok = 0; tok < T; ++tok)
-      for (int v = threadIdx.x; v < units; v += 32 * active) {
-        const uint4 d =
-            v < have ? reinterpret_cast<const uint4*>(x + (long long)tok * K)[v] : make_uint4(0u, 0u, 0u, 0u);
-        // unit 8 t + q of a panel lies at 4 q + t: the lanes of a fragment's load read 64 consecutive bytes a token
-        *reinterpret_cast<uint4*>(held + tok * x_pitch + ((v & ~31) + 4 * (v & 7) + (v >> 3 & 3)) * 16) = d;
-      }
+  float acc[kChains][NT][4] = {};
+  const uint4* x4[NT];  // columns past T are dropped: whatever token their fragments hold
 #pragma unroll
-    for (int m = 0; m < NT; ++m) xs[m] = (uint32_t)(held - smem) + min(g + 8 * m, T - 1) * x_pitch + 16 * t;
-    __syncwarp();
-    asm volatile("bar.sync 15, %0;" ::"r"(32 * active) : "memory");
-  }
-  // 16-byte units 2 t and 2 t + 1 of a row's 128 bytes, swizzled by the row (its last three bits are g's)
-  const uint32_t even = ring_at + g * (kPanel / 2) + ((2 * t) ^ g) * 16;
-  const uint32_t odd = ring_at + g * (kPanel / 2) + ((2 * t + 1) ^ g) * 16;
-  bool waited = !b.after_su, alive = true;
-  int s = 0, proj = 0;
-  uint32_t phase = 0;
-  for (int tile = slot; tile < cut.tiles; tile += slots) {
-    while (proj + 1 < b.n && tile >= b.p[proj + 1].tile_begin) ++proj;
-    const DecodeProj& p = b.p[proj];
-    const int n0 = (tile - p.tile_begin) * kRows, r = p.r;
-    // the adapter's A operand of 16 columns: rows g and g + 8 of B, columns 2 t (+ 1) and 2 t + 8 (+ 9)
-    auto load_adapter = [&](int mt, int j0, uint32_t (&a)[4]) {
+  for (int m = 0; m < NT; ++m)
+    x4[m] = reinterpret_cast<const uint4*>(p.x + (long long)min(g + 8 * m, T - 1) * K + 32 * t);
+  for (int c = warp; c * kChunk < K; c += warps) {
+    const uint32_t pa = dq40_pair(s.s0), pb = dq40_pair(s.s1);
+    const uint32_t sa = __byte_perm(pa, 0u, 0x1010), ba = __byte_perm(pa, 0u, 0x3232), sa4 = dq40_high(sa);
+    const uint32_t sb = __byte_perm(pb, 0u, 0x1010), bb = __byte_perm(pb, 0u, 0x3232), sb4 = dq40_high(sb);
+    const uint32_t u0[4] = {s.w0.x, s.w0.y, s.w0.z, s.w0.w}, u1[4] = {s.w1.x, s.w1.y, s.w1.z, s.w1.w};
+    const bool in = c * kChunk + 32 * t < K;
+    uint4 xv[NT][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int n = n0 + mt * kTileN + g + 8 * (i & 1), j = j0 + 2 * t + 8 * (i >> 1);
-        const uint16_t* q = reinterpret_cast<const uint16_t*>(p.B) + (long long)n * r + j;
-        a[i] = 0u;
-        if (n < p.N && j < r) {
-          if (r % 2 == 0)
-            a[i] = __ldg(reinterpret_cast<const uint32_t*>(q));
-          else
-            a[i] = __ldg(q) | (j + 1 < r ? (uint32_t)__ldg(q + 1) << 16 : 0u);
-        }
-      }
-    };
-    uint32_t adapter[MT][4];  // its first columns, on their way meanwhile
+    for (int m = 0; m < NT; ++m)
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) load_adapter(mt, 16 * wg, adapter[mt]);
-    float acc[kChains][MT][NT][4] = {};
-    for (int c = wg; c < panels; c += split) {
-      uint32_t sc[MT][2], sc4[MT][2], of[MT][2];
+      for (int q = 0; q < 4; ++q) xv[m][q] = in ? __ldg(x4[m] + c * (kChunk / 8) + q) : make_uint4(0u, 0u, 0u, 0u);
+    fetch(s, c + warps);
 #pragma unroll
-      for (int i = 0; i < 2 * MT; ++i) {  // eights of rows
-        const uint32_t sb = mul_bf16x2(next_pair[i], 0x2B806E00u);  // 2^93, 2^-40
-        sc[i / 2][i % 2] = __byte_perm(sb, 0u, 0x1010);
-        of[i / 2][i % 2] = __byte_perm(sb, 0u, 0x3232);
-        sc4[i / 2][i % 2] = mul_bf16x2(sc[i / 2][i % 2], 0x3D803D80u);  // 1/16
-      }
-      fetch_pairs();
-      if (alive) alive = mbar_wait(bar + 8 * s, phase, wait, abort);
-      __syncwarp();  // the MMAs need the warp whole
-      const uint32_t at = s * kStageBytes, xc = c * (kPanel * 2);
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {  // a lane's first 32 columns and its last
-        uint4 w[MT][2];
-#pragma unroll
-        for (int i = 0; i < 2 * MT; ++i)
-          w[i / 2][i % 2] = *reinterpret_cast<const uint4*>(smem + at + (half ? odd : even) + i * 8 * (kPanel / 2));
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint4 xv[NT];
-#pragma unroll
-          for (int m = 0; m < NT; ++m) {
-            if (XS)
-              xv[m] = *reinterpret_cast<const uint4*>(smem + xs[m] + xc + 256 * half + 64 * q);
-            else
-              xv[m] = 4 * c + t < pairs ? __ldg(reinterpret_cast<const uint4*>(
-                                              x + (long long)min(g + 8 * m, T - 1) * K + c * kPanel + 64 * t + 32 * half +
-                                              8 * q))
-                                        : make_uint4(0u, 0u, 0u, 0u);
-          }
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            const uint4 w0 = w[mt][0], w1 = w[mt][1];
-            const uint32_t u0 = q == 0 ? w0.x : q == 1 ? w0.y : q == 2 ? w0.z : w0.w;
-            const uint32_t u1 = q == 0 ? w1.x : q == 1 ? w1.y : q == 2 ? w1.z : w1.w;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint32_t v0 = h ? u0 >> 8 : u0, v1 = h ? u1 >> 8 : u1;
-              const uint32_t a0 = fma_bf16x2(v0 & 0x000F000Fu, sc[mt][0], of[mt][0]);
-              const uint32_t a1 = fma_bf16x2(v1 & 0x000F000Fu, sc[mt][1], of[mt][1]);
-              const uint32_t a2 = fma_bf16x2(v0 & 0x00F000F0u, sc4[mt][0], of[mt][0]);
-              const uint32_t a3 = fma_bf16x2(v1 & 0x00F000F0u, sc4[mt][1], of[mt][1]);
-#pragma unroll
-              for (int m = 0; m < NT; ++m)
-                mma_bf16(acc[h % kChains][mt][m], a0, a1, a2, a3, h ? xv[m].z : xv[m].x, h ? xv[m].w : xv[m].y);
-            }
-          }
-        }
-      }
-      __syncwarp();
-      if (lane == 0 && alive) issue(s);
-      if (++s == cut.stages) {
-        s = 0;
-        phase ^= 1u;
-      }
-    }
-    if (kChains == 2) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[0][0][0][e] += acc[kChains - 1][0][0][e];
-    }
-    for (int j0 = 16 * wg; j0 < r; j0 += 16 * split) {
-      if (!waited) {
-        griddep_wait();  // su
-        waited = true;
-      }
-      uint4 lo[NT], hi[NT];
+    for (int q = 0; q < 4; ++q) {
+      uint32_t a[2][4];
+      dq40_word(u0[q], sa, sa4, ba, a[0][0], a[0][2], a[1][0], a[1][2]);
+      dq40_word(u1[q], sb, sb4, bb, a[0][1], a[0][3], a[1][1], a[1][3]);
 #pragma unroll
       for (int m = 0; m < NT; ++m) {
-        const uint4* su =
-            reinterpret_cast<const uint4*>(p.su + (min(g + 8 * m, T - 1) * su_steps(r) + j0 / 16) * kSuWords + 8 * t);
-        lo[m] = su[0];
-        hi[m] = su[1];
-      }
-      __syncwarp();
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        if (j0 != 16 * wg) load_adapter(mt, j0, adapter[mt]);
-        __syncwarp();
-        const uint32_t(&a)[4] = adapter[mt];
-#pragma unroll
-        for (int m = 0; m < NT; ++m) {
-          mma_bf16(acc[0][mt][m], a[0], a[1], a[2], a[3], lo[m].x, hi[m].x);
-          mma_bf16(acc[0][mt][m], a[0], a[1], a[2], a[3], lo[m].y, hi[m].y);
-          mma_bf16(acc[0][mt][m], a[0], a[1], a[2], a[3], lo[m].z, hi[m].z);
-        }
-      }
-    }
-    auto sync_group = [&]() {
-      __syncwarp();  // a warp in parts would count as several
-      asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(32 * split) : "memory");
-    };
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      if (split == 1) {
-#pragma unroll
-        for (int m = 0; m < NT; ++m)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int tok = 8 * m + 2 * t + (e & 1), n = n0 + mt * kTileN + g + 8 * (e >> 1);
-            if (tok < T && n < p.N) p.y[(long long)tok * p.N + n] = __float2bfloat16(acc[0][mt][m][e] * 0x1p40f);
-          }
-        continue;
-      }
-      float* red = reinterpret_cast<float*>(red_at);  // [active][NT * 8][kRedPitch]
-      float* mine = red + warp * (NT * 8 * kRedPitch);
-      sync_group();  // the sums of the tile before are read
-#pragma unroll
-      for (int m = 0; m < NT; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) mine[(8 * m + 2 * t + (e & 1)) * kRedPitch + g + 8 * (e >> 1)] = acc[0][mt][m][e];
-      sync_group();
-      const float* sums = red + group * split * (NT * 8 * kRedPitch);
-      for (int o = wg * 32 + lane; o < kTileN * T; o += 32 * split) {
-        const int tok = o / kTileN, row = o % kTileN, n = n0 + mt * kTileN + row;
-        float v = 0.f;
-#pragma unroll 4
-        for (int w = 0; w < split; ++w) v += sums[(w * NT * 8 + tok) * kRedPitch + row];
-        if (n < p.N) p.y[(long long)tok * p.N + n] = __float2bfloat16(v * 0x1p40f);
+        mma_bf16(acc[0][m], a[0][0], a[0][1], a[0][2], a[0][3], xv[m][q].x, xv[m][q].y);
+        mma_bf16(acc[kChains - 1][m], a[1][0], a[1][1], a[1][2], a[1][3], xv[m][q].z, xv[m][q].w);
       }
     }
   }
-  if (!waited) griddep_wait();  // no grid ends before the ones it follows
-  // a wait gave up: the warp's copies still in flight land before the shared memory is released (bounded)
-  if (!alive && lane == 0)
-    for (int i = issued - 1; i >= 0 && i >= issued - cut.stages; --i)
-      mbar_wait_drain(bar + 8 * (i % cut.stages), (uint32_t)((i / cut.stages) & 1), kAbortDrainNs);
-}
-
-int tiles_of(const DecodeProj& p, int mt) { return (p.N + mt * kTileN - 1) / (mt * kTileN); }
-int panels_of(const DecodeProj& p) { return (p.K + kPanel - 1) / kPanel; }
-
-// The cheapest cut, in clocks of an SM: the instructions of its tiles at the rate that its warps reach, or the longest
-// warp's path, whichever takes longer.
-bool choose_cut(const DecodeBatch& b, int nt, int mt, bool xs, int num_sms, Cut* best, double* least) {
-  const DecodeProj& p = b.p[0];
-  const int panels = panels_of(p);
-  int tiles = 0;
-  for (int i = 0; i < b.n; ++i) tiles += tiles_of(b.p[i], mt);
-  const int per_sm = (tiles + num_sms - 1) / num_sms;
-  bool found = false;
-  for (int split : {1, 2, 3, 4, 6, 8, 12, 16}) {
-    if (split > panels) break;
-    int last = 0;
-    for (int rounds = (per_sm * split + kWarps - 1) / kWarps; rounds <= per_sm; ++rounds) {
-      Cut c;
-      c.split = split;
-      c.tiles = tiles;
-      c.groups = (per_sm + rounds - 1) / rounds;
-      if (c.groups == last) continue;
-      last = c.groups;
-      const int active = c.groups * split;
-      if (active < 8 && rounds > 1) break;
-      c.red_bytes = split > 1 ? active * nt * 8 * kRedPitch * 4 : 0;
-      c.held_bytes = xs ? (p.T * (panels * (kPanel * 2) + kXPad) + 127) & ~127 : 0;
-      const int room = kMostSmem - kCtlBytes - c.red_bytes - c.held_bytes;
-      c.stages = std::min(std::min(kMaxStages, (panels + split - 1) / split * rounds),
-                          room / (active * (mt * kTileN * (kPanel / 2) + 8)));
-      if (c.stages < std::min(2, (panels + split - 1) / split * rounds)) continue;
-      const double rate = std::min(2.7, (mt == 1 ? 0.17 : 0.2) * active);
-      const double step = (nt == 1 ? 205 : mt == 1 ? 240 : 220) * mt;
-      const double work = per_sm * (panels * step + (split > 1 ? 100.0 * split : 60.0) * mt) / rate;
-      const double path = (double)rounds * ((panels + split - 1) / split) * mt * 500;
-      const double cost = std::max(work, path) + rounds * (split > 1 ? 300.0 : 100.0);
-      if (cost < *least) {
-        *least = cost;
-        *best = c;
-        found = true;
-      }
+  if (b.after_su) griddep_wait();  // su
+  for (int j0 = 16 * warp; j0 < r; j0 += 16 * warps) {
+    if (j0 != 16 * warp) load_adapter(j0, adapter);
+    __syncwarp();
+#pragma unroll
+    for (int m = 0; m < NT; ++m) {
+      const uint4* su =
+          reinterpret_cast<const uint4*>(p.su + (min(g + 8 * m, T - 1) * su_steps(r) + j0 / 16) * kSuWords + 8 * t);
+      const uint4 lo = su[0], hi = su[1];
+      mma_bf16(acc[0][m], adapter[0], adapter[1], adapter[2], adapter[3], lo.x, hi.x);
+      mma_bf16(acc[kChains - 1][m], adapter[0], adapter[1], adapter[2], adapter[3], lo.y, hi.y);
+      mma_bf16(acc[0][m], adapter[0], adapter[1], adapter[2], adapter[3], lo.z, hi.z);
     }
   }
-  return found;
+  __shared__ float red[kMostThreads / 32][NT * 8][kRedPitch];
+#pragma unroll
+  for (int m = 0; m < NT; ++m)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      red[warp][8 * m + 2 * t + (e & 1)][g + 8 * (e >> 1)] = kChains == 2 ? acc[0][m][e] + acc[kChains - 1][m][e] : acc[0][m][e];
+  __syncthreads();
+  for (int o = threadIdx.x; o < kTileN * T; o += blockDim.x) {
+    const int tok = o / kTileN, row = o % kTileN, n = n0 + row;
+    float v = 0.f;
+    for (int w = 0; w < warps; ++w) v += red[w][tok][row];
+    if (n < p.N) p.y[(long long)tok * p.N + n] = __float2bfloat16(v * 0x1p40f);
+  }
 }
 
-template <int NT, int MT, bool XS>
-cudaError_t launch_main(DecodeBatch& b, const Cut& cut, int num_sms, cudaStream_t st) {
-  static std::atomic<unsigned long long> done{0};
-  const cudaError_t e = set_smem_once(decode_kernel<NT, MT, XS>, kMostSmem, done);
-  if (e != cudaSuccess) return e;
-  int begin = 0;
+cudaError_t launch_narrow(DecodeBatch& b, int most, int num_sms, cudaStream_t st) {
+  int tiles = 0, chunks = 1;
   for (int i = 0; i < b.n; ++i) {
-    DecodeProj& p = b.p[i];
-    p.tile_begin = begin;
-    begin += tiles_of(p, MT);
-    if (!make_codes_map(&b.codes[i], p.codes, p.K / 2, p.N, kPanel / 2, MT * kTileN)) return cudaErrorInvalidValue;
+    b.p[i].tile_begin = tiles;
+    tiles += (b.p[i].N + kTileN - 1) / kTileN;
+    chunks = std::max(chunks, (b.p[i].K + kChunk - 1) / kChunk);
   }
-  const int active = cut.groups * cut.split;
-  const size_t smem = (size_t)active * cut.stages * (MT * kTileN * (kPanel / 2) + 8) + cut.red_bytes + cut.held_bytes + kCtlBytes;
-  return launch_kernel(decode_kernel<NT, MT, XS>, dim3(std::min(cut.tiles, num_sms)), dim3(kThreads), smem, st, 1, b, cut);
-}
-
-template <int NT>
-cudaError_t launch_main(DecodeBatch& b, int num_sms, cudaStream_t st) {
-  Cut cut;
-  double least = 1e300;
-  const bool one = choose_cut(b, NT, 1, true, num_sms, &cut, &least);
-  if (choose_cut(b, NT, 2, true, num_sms, &cut, &least)) return launch_main<NT, 2, true>(b, cut, num_sms, st);
-  if (one) return launch_main<NT, 1, true>(b, cut, num_sms, st);
-  if (!choose_cut(b, NT, 1, false, num_sms, &cut, &least)) return cudaErrorInvalidConfiguration;
-  return launch_main<NT, 1, false>(b, cut, num_sms, st);
+  // The steps of a warp, and about a quarter of one for each warp that a block's sums come from, times the waves of
+  // blocks (about 30 warps fit an SM).  (3072 x 5120: 8 warps 5.4, 4: 6.7 us; 8192 x 3072: 16: 7.5, 8: 8.5, 4: 12.6 us;
+  // 2048 x 11008: 4: 6.1, 8: 7.6, 2: 8.0 us)
+  int warps = 1;
+  double least = 0.0;
+  for (int w = 1; w <= kMostThreads / 32 && w <= chunks; ++w) {
+    const long long waves = ((long long)tiles * w + 30 * num_sms - 1) / (30 * num_sms);
+    const double cost = (double)waves * ((chunks + w - 1) / w + 0.25 * w);
+    if (w == 1 || cost < least) {
+      warps = w;
+      least = cost;
+    }
+  }
+  return most <= 8 ? launch_kernel(decode_kernel<1>, dim3(tiles), dim3(32 * warps), 0, st, 1, b)
+                   : launch_kernel(decode_kernel<2>, dim3(tiles), dim3(32 * warps), 0, st, 1, b);
 }
 
 cudaError_t launch_su(const DecodeBatch& b, int most, cudaStream_t st) {
@@ -472,9 +261,36 @@ cudaError_t launch_su(const DecodeBatch& b, int most, cudaStream_t st) {
   return launch_kernel(su, dim3(b.rows), dim3(kSuThreads), 0, st, 1, b);
 }
 
+// Which second launch a group of projections takes, by their times as measured (us): 16-row blocks read their bytes at
+// 4.3 TB/s for one token, 3 for eight and 1.8 for sixteen, and are there at once; the wide launch takes 0.475 for a
+// panel of 128 rows whatever the tokens, and starts late.  (3072 x 128256, 1 and 16 tokens: blocks 52 and 117, wide 44
+// and 45; 3072 x 16384: 9.0 and 19, 10.9 and 11.3; 8192 x 3072: 8.4 and 13.7, 19 and 20; 4096 x 16384, 8 tokens: 15.5,
+// 13.0.)
+bool wide_pays(const DecodeBatch& b, int num_sms) {
+  const int T = b.p[0].T, K = b.p[0].K;
+  double mb = 0.0;
+  long long tiles = 0;
+  int adapters = 0;
+  for (int i = 0; i < b.n; ++i) {
+    mb += (double)b.p[i].N * K * (0.5625e-6);
+    tiles += (b.p[i].N + 127) / 128;
+    adapters |= b.p[i].r > 0;
+  }
+  const double blocks = 2.6 + mb * (T <= 8 ? 0.22 + 0.0155 * T : 0.27 + 0.018 * T);
+  const double wide = 4.6 + (double)((tiles + num_sms - 1) / num_sms) * ((K + 255) / 256 + adapters) * 0.475;
+  return wide < blocks;
+}
+
 }  // namespace
 
-size_t decode_su_bytes(int64_t T, int64_t r) { return (size_t)T * su_steps((int)r) * kSuWords * 4; }
+size_t decode_su_bytes(int64_t T, int64_t r) {
+  return (size_t)T * su_steps((int)r) * kSuWords * 4 + (size_t)kSuTerms * su_blocks((int)r) * kSuBlock;
+}
+
+void set_decode_su(DecodeProj& p, void* at) {
+  p.su = static_cast<uint32_t*>(at);
+  p.su_image = static_cast<uint8_t*>(at) + (size_t)p.T * su_steps(p.r) * kSuWords * 4;
+}
 
 cudaError_t launch_decode(DecodeBatch& b, int num_sms, cudaStream_t st) {
   b.rows = 0;
@@ -488,24 +304,31 @@ cudaError_t launch_decode(DecodeBatch& b, int num_sms, cudaStream_t st) {
     const cudaError_t e = launch_su(b, most, st);
     if (e != cudaSuccess) return e;
   }
-  // one launch for the projections that read one activation: q, k and v; gate and up
+  // projections of many rows: one launch for those that read one activation (gate and up); one for all the others
+  DecodeBatch rest, same;
+  rest.n = 0;
+  rest.after_su = same.after_su = b.rows > 0;
+  rest.status = same.status = b.status;
+  rest.limit_ns = same.limit_ns = b.limit_ns;
   bool taken[kDecodeMaxProjs] = {};
+  most = 1;
   for (int i = 0; i < b.n; ++i) {
     if (taken[i]) continue;
-    DecodeBatch same;
     same.n = 0;
-    same.after_su = b.rows > 0;
-    same.status = b.status;
-    same.limit_ns = b.limit_ns;
     for (int j = i; j < b.n; ++j) {
       if (taken[j] || b.p[j].x != b.p[i].x || b.p[j].T != b.p[i].T || b.p[j].K != b.p[i].K) continue;
       taken[j] = true;
       same.p[same.n++] = b.p[j];
     }
-    const cudaError_t e = b.p[i].T <= 8 ? launch_main<1>(same, num_sms, st) : launch_main<2>(same, num_sms, st);
-    if (e != cudaSuccess) return e;
+    if (wide_pays(same, num_sms)) {
+      const cudaError_t e = launch_decode_wide(same, num_sms, st);
+      if (e != cudaSuccess) return e;
+    } else {
+      for (int j = 0; j < same.n; ++j) rest.p[rest.n++] = same.p[j];
+      most = std::max(most, b.p[i].T);
+    }
   }
-  return cudaSuccess;
+  return rest.n ? launch_narrow(rest, most, num_sms, st) : cudaSuccess;
 }
 
 }  // namespace lora

@@ -403,7 +403,9 @@ struct DecodeProj {
   const __nv_bfloat16* A;       // [r, K]
   const __nv_bfloat16* B;       // [N, r]
   __nv_bfloat16* y;             // [T, N]
-  uint32_t* su;                 // decode_su_bytes(T, r): scale * x A^T, written by the first launch
+  // scale * x A^T, written by the first launch (set_decode_su), as the operand of either second launch's MMAs
+  uint32_t* su;
+  uint8_t* su_image;
   float scale;
   int T, N, K, r;
   int tile_begin;  // first of its row tiles in the launch's list
@@ -419,12 +421,26 @@ struct DecodeBatch {
   long long limit_ns;
 };
 
+// su times 2^-40 (like the weights, dq40_word) is held as three bf16 terms, all 24 bits of its fp32 value, zeros
+// behind column r:
+//   su        for 16 adapter columns at a time: [T][su_steps(r)][t = 0..3][8 words], where words 0..2 hold columns 2 t
+//             and 2 t + 1 in the terms, and words 4..6 columns 2 t + 8 and 2 t + 9
+//   su_image  [term][64 adapter columns][16 tokens][128 bytes], 16-byte units swizzled by the token: a K-major operand of
+//             tcgen05 (rows past T hold nothing)
+constexpr int kSuTerms = 3, kSuWords = 32, kSuBlock = 2048;
+__host__ __device__ constexpr int su_steps(int r) { return (r + 15) / 16; }
+__host__ __device__ constexpr int su_blocks(int r) { return (r + 63) / 64; }
 size_t decode_su_bytes(int64_t T, int64_t r);
+void set_decode_su(DecodeProj& p, void* at);  // T and r are set
 // Tensor map of a matrix of bytes [rows, width] for boxes of box_width (128) x box_rows, 128-byte swizzle, zeros outside.
-bool make_codes_map(CUtensorMap* m, const void* ptr, int width, int rows, int box_width, int box_rows);
+bool make_bytes_map(CUtensorMap* m, const void* ptr, int width, int rows, int box_width, int box_rows);
+// The same of a bf16 matrix for boxes of 64 columns (128 bytes).
+bool make_bf16_map(CUtensorMap* m, const void* ptr, int width, int rows, int box_width, int box_rows);
 // su of every projection with an adapter (nothing to launch without one), then y = x W^T + su B^T.  The caller
 // sets all but the begins and the totals.
 cudaError_t launch_decode(DecodeBatch& b, int num_sms, cudaStream_t stream);
+// Its second launch for many rows (decode_wide.cu), of projections with one activation.
+cudaError_t launch_decode_wide(DecodeBatch& b, int num_sms, cudaStream_t stream);
 
 // ---------------------------------------------------------------- policy and preference losses
 struct ObjectiveSeq {  // what the first launch leaves per sequence (policy) or pair (preference), sums as fp32 pairs

@@ -178,7 +178,8 @@ def test_same_bits_every_time_and_on_another_stream():
 
 
 @pytest.mark.parametrize("T,K,N", [(16, 3072, 30000), (16, 1024, 20001), (8, 3072, 30000), (9, 320, 50000),
-                                   (16, 6144, 6000), (3, 11008, 2048), (16, 12288, 1000)])
+                                   (16, 6144, 6000), (3, 11008, 2048), (16, 12288, 1000), (16, 4416, 40001),
+                                   (13, 64, 200003)])
 def test_many_tiles_come_out_the_same_in_every_call(T, K, N):
     """Every SM takes many tiles through its rings, with little room for them beside 16 tokens: 100 calls, bit for
     bit, and against the product in fp32."""
@@ -234,6 +235,45 @@ def test_chain_of_calls_in_a_graph():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(c.y, want) and not torch.equal(want, torch.zeros_like(want))
+
+
+@pytest.mark.parametrize("T,K,shapes", [
+    (16, 1024, [(40001, 16), (30000, 0), (129, 128), (2500, 13)]), (1, 4160, [(90001, 64)]), (9, 192, [(150000, 1), (7, 3)]),
+    (12, 8192, [(20011, 128), (20000, 0)])])
+def test_many_rows_with_adapters(T, K, shapes):
+    """Projections of tens of thousands of rows that share an activation, with adapters of any rank or none: the
+    launch for many rows, against fp32 products (the bound of the module's head, twice the sums' part)."""
+    g = torch.Generator(device="cuda").manual_seed(K + T)
+    sd = K ** -0.5
+    x = torch.randn(T, K, generator=g, device="cuda").to(torch.bfloat16)
+    shift = torch.tensor([[0, 16], [4, 20], [8, 24], [12, 28]], device="cuda", dtype=torch.int32)
+    projs, check = [], []
+    for N, r in shapes:
+        codes = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+        s = torch.empty(N, K // 64, device="cuda").uniform_(0.2, 0.45, generator=g) * sd
+        params = torch.stack([s, -7.5 * s], dim=-1).to(torch.bfloat16).contiguous()
+        A = (torch.randn(r, K, generator=g, device="cuda") * sd).to(torch.bfloat16) if r else None
+        B = (torch.randn(N, r, generator=g, device="cuda") * 0.1).to(torch.bfloat16) if r else None
+        out = torch.full((GUARD + T * N + GUARD,), 77.0, dtype=torch.bfloat16, device="cuda")
+        projs.append(lora.make_proj(lora.make_shape(T, K, N, r, 2.0), x=x, A=A, B=B, y=out[GUARD:],
+                                    Wq=lora.make_q4(codes, params)))
+        check.append((N, codes, params, A, B, out))
+    projs = lora.make_projs(projs)
+    ws = G.workspace(lora.lora_decode_workspace_size(projs))
+    for _ in range(3):
+        lora.lora_decode_q4(projs, ws, ws.numel())
+    torch.cuda.synchronize()
+    assert lora.lora_read_status() == lora.LORA_OK
+    for N, codes, params, A, B, out in check:
+        q = ((codes.view(torch.int32)[:, :, None, None] >> shift) & 15).float().view(N, K // 64, 64)
+        W = (params[:, :, :1].float() * q + params[:, :, 1:].float()).to(torch.bfloat16).float().view(N, K)
+        want, size = x.float() @ W.T, x.float().abs() @ W.abs().T
+        if A is not None:
+            want = want + 2.0 * (x.float() @ A.float().T) @ B.float().T
+            size = size + 2.0 * (x.float().abs() @ A.float().abs().T) @ B.float().abs().T
+        y = out[GUARD:GUARD + T * N].view(T, N).float()
+        assert ((y - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -19 * size).all()
+        assert (out[:GUARD] == 77).all() and (out[GUARD + T * N:] == 77).all()
 
 
 def test_codes_past_two_to_the_32_bytes():

@@ -62,7 +62,7 @@ def test_decode_workspace():
     assert lora.lora_decode_workspace_size(proj(r=0, A=None, B=None)) == 0
     assert code(lora.lora_decode_q4, proj(), None, 0, 0) == lora.LORA_EWORKSPACE
     assert code(lora.lora_decode_q4, proj(), P, 16, 0) == lora.LORA_EWORKSPACE
-    assert code(lora.lora_decode_q4, proj(), P + 16, 4096, 0) == lora.LORA_EALIGN
+    assert code(lora.lora_decode_q4, proj(), P + 16, 1 << 20, 0) == lora.LORA_EALIGN
     n = ctypes.c_size_t(0)
     assert lora.library().lora_decode_workspace_size(None, 1, ctypes.byref(n)) == lora.LORA_ENULL
     assert lora.library().lora_decode_workspace_size(proj(), 0, ctypes.byref(n)) == lora.LORA_EINVAL
