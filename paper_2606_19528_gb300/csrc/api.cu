@@ -2187,7 +2187,7 @@ int clip_batches(const lora_grad* grads, int n, int* partials, Launch launch) {
   for (int i = 0; i < n; ++i) {
     const lora_grad& g = grads[i];
     if (!g.n) continue;
-    const int chunks = cdiv(g.n, kClipChunk);  // at most 2^29
+    const int chunks = cdiv(g.n, kClipChunk);  // at most 2^28
     if ((b.n == kClipTensors || b.chunks > (1 << 30)) && (rc = flush()) != LORA_OK) return rc;
     ClipTensor& t = b.t[b.n++];
     t.src = g.src;

@@ -1,10 +1,11 @@
 // Global norm of many gradient tensors, and their clipping to a bound:
 //   norm = sqrt(sum g^2),  coef = norm > max_norm ? max_norm / norm : 1,  dst = coef * src
 //
-// A warp takes a piece of 512 elements (2 KB of fp32) at a time, the next one's loads issued before it is used; the
-// pieces are dealt to the CTAs in equal contiguous runs.  Small calls run as one launch, many tensors as two:
-//   clip_one_kernel    one cluster, two pieces per warp: the elements stay in registers between the sum and the
-//                      scaling, the CTAs exchange their sums through distributed shared memory
+// A warp takes a piece of 1024 elements (4 KB of fp32) at a time, in two halves, the next half's loads issued before
+// one is used; the pieces are dealt to the CTAs in equal contiguous runs.  Small calls run as one launch, many tensors
+// as two:
+//   clip_one_kernel    one cluster, a piece per warp: the elements stay in registers between the sum and the scaling,
+//                      the CTAs exchange their sums through distributed shared memory
 //   clip_sum_kernel    the CTAs' sums of squares, one CTA per SM
 //   clip_scale_kernel  every CTA adds these up again in the same order, then scales, from the last piece to the first:
 //                      what was read last is still in L2
@@ -22,7 +23,8 @@ namespace lora {
 namespace {
 
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
-constexpr int kOneCtas = 8, kOnePieces = 2;  // of the single cluster; a warp's pieces in it
+constexpr int kScaleWarps = 16;  // of the scaling, one CTA per SM: their registers hold what is on its way
+constexpr int kOneCtas = 16;  // of the single cluster
 
 // A piece's place: the elements before the first 16-byte boundary of src (head), the vectors behind them, the rest.
 struct Piece {
@@ -60,9 +62,9 @@ __device__ __forceinline__ int find_tensor(const Table& b, int c) {
   return lo;
 }
 
-constexpr int kVecs = kClipChunk / 4 / 32;  // 16-byte vectors of a lane (fp32; half of them with bf16)
+constexpr int kVecs = kClipChunk / 8 / 32;  // 16-byte vectors of a lane in half a piece (all of it with bf16)
 
-// A lane's part of a piece: vectors lane, lane + 32, ..; one element of the head or of the rest.
+// A lane's part of half a piece: every 32nd vector; with the first half, an element of the head or of the rest.
 struct Held {
   uint4 v[kVecs];
   uint32_t edge;  // as fp32
@@ -74,16 +76,19 @@ __device__ __forceinline__ int edge_index(const Piece& p, int lane) {
   return i < p.n ? i : -1;
 }
 
+template <int PART>
 __device__ __forceinline__ void load_piece(const Piece& p, int lane, Held& h) {
-  const uint4* v = reinterpret_cast<const uint4*>(p.src + (p.head << (p.half ? 1 : 2)));
+  const uint4* v = reinterpret_cast<const uint4*>(p.src + (p.head << (p.half ? 1 : 2))) + lane + 32 * kVecs * PART;
+  const int left = p.vecs - lane - 32 * kVecs * PART;
 #pragma unroll
-  for (int q = 0; q < kVecs; ++q)
-    h.v[q] = lane + 32 * q < p.vecs ? v[lane + 32 * q] : make_uint4(0u, 0u, 0u, 0u);
-  const int e = edge_index(p, lane);
+  for (int q = 0; q < kVecs; ++q) h.v[q] = 32 * q < left ? v[32 * q] : make_uint4(0u, 0u, 0u, 0u);
   h.edge = 0u;
-  if (e >= 0)
-    h.edge = p.half ? (uint32_t) reinterpret_cast<const uint16_t*>(p.src)[e] << 16
-                    : reinterpret_cast<const uint32_t*>(p.src)[e];
+  if (PART == 0) {
+    const int e = edge_index(p, lane);
+    if (e >= 0)
+      h.edge = p.half ? (uint32_t) reinterpret_cast<const uint16_t*>(p.src)[e] << 16
+                      : reinterpret_cast<const uint32_t*>(p.src)[e];
+  }
 }
 
 __device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
@@ -98,7 +103,7 @@ __device__ __forceinline__ float squares(const Held& h, float scale) {
   };
   float s[4] = {of(__uint_as_float(h.edge), 0.f), 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int q = 0; q < (HALF ? kVecs / 2 : kVecs); ++q) {
+  for (int q = 0; q < kVecs; ++q) {
     const uint32_t w[4] = {h.v[q].x, h.v[q].y, h.v[q].z, h.v[q].w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -113,52 +118,56 @@ __device__ __forceinline__ float squares(const Held& h, float scale) {
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-// The same of a piece that is loaded again, for the rare sums that need it.
-__device__ __noinline__ float squares_scaled(const uint8_t* src, int n, int head, int vecs, bool half, float scale) {
-  Piece p;
-  p.src = src;
-  p.n = n;
-  p.head = head;
-  p.vecs = vecs;
-  p.half = half;
-  Held h;
-  load_piece(p, threadIdx.x & 31, h);
-  return half ? squares<true, true>(h, scale) : squares<false, true>(h, scale);
-}
-
-// A lane's sum of squares: `most` holds those that fp32 forms without loss, `rest` what it cannot (below 2^-60, where
-// squares may have been lost, or beyond 2^100), from elements scaled by a power of two: 2^60 twice brings the
-// smallest subnormal's square into range, 2^-80 the largest element's.
+// A lane's sum of squares, where fp32 forms them without loss: each half piece's sum between 2^-60 and 2^100, or of
+// zeros alone.  Elsewhere `lost` is set, and slow_squares() takes all of the warp's pieces again.
 struct Squares {
-  Pair most{};
-  double rest = 0.0;
+  Pair sum{};
+  bool lost = false;
   __device__ __forceinline__ void add(const Piece& p, const Held& h) {
-    float s = p.half ? squares<true, false>(h, 1.f) : squares<false, false>(h, 1.f);
+    const float s = p.half ? squares<true, false>(h, 1.f) : squares<false, false>(h, 1.f);
     if (s >= 0x1p-60f && s <= 0x1p100f) {
-      most.add(s);
+      sum.add(s);
       return;
     }
-    double unit = 0x1p160;
-    if (s < 0x1p-60f) {
-      s = squares_scaled(p.src, p.n, p.head, p.vecs, p.half, 0x1p60f);
-      unit = 0x1p-120;
-      if (s < 0x1p-60f) {
-        s = squares_scaled(p.src, p.n, p.head, p.vecs, p.half, 0x1p120f);
-        unit = 0x1p-240;
-      }
-      if (s == 0.f) return;
-    } else {
-      s = squares_scaled(p.src, p.n, p.head, p.vecs, p.half, 0x1p-80f);
-    }
-    rest += (double)s * unit;
-  }
-  // over the warp's lanes
-  __device__ __forceinline__ double total() const {
-    double v = warp_sum(most).wide();
-    if (__any_sync(0xffffffffu, rest != 0.0)) v += warp_sum(rest);
-    return v;
+    uint32_t any = h.edge;
+#pragma unroll
+    for (int q = 0; q < kVecs; ++q) any |= h.v[q].x | h.v[q].y | h.v[q].z | h.v[q].w;
+    lost = lost || s != 0.f || (any & 0x7fff7fffu) != 0u;
   }
 };
+
+// Half a piece's squares from elements scaled by a power of two: 2^60 twice brings the smallest subnormal's square into
+// fp32's range, 2^-80 the largest element's.
+__device__ __forceinline__ double scaled_squares(const Held& h, bool half) {
+  auto of = [&](float scale) { return half ? squares<true, true>(h, scale) : squares<false, true>(h, scale); };
+  float s = of(1.f);
+  if (s >= 0x1p-60f && s <= 0x1p100f) return (double)s;
+  if (!(s < 0x1p-60f)) return (double)of(0x1p-80f) * 0x1p160;
+  s = of(0x1p60f);
+  return s >= 0x1p-60f ? (double)s * 0x1p-120 : (double)of(0x1p120f) * 0x1p-240;
+}
+
+// A lane's sum over pieces c, c + kWarps, .. below c1, whatever the elements.
+template <typename Table>
+__device__ __noinline__ double slow_squares(const Table& b, int c, int c1) {
+  const int lane = threadIdx.x & 31;
+  double sum = 0.0;
+  for (; c < c1; c += kWarps) {
+    const Piece p = piece_of(b.t[find_tensor(b, c)], c);
+    Held h;
+    load_piece<0>(p, lane, h);
+    sum += scaled_squares(h, p.half);
+    load_piece<1>(p, lane, h);
+    sum += scaled_squares(h, p.half);
+  }
+  return sum;
+}
+
+// The warp's sum over its pieces c, c + kWarps, .. below c1.
+template <typename Table>
+__device__ __forceinline__ double warp_total(const Squares& s, const Table& b, int c, int c1) {
+  return __any_sync(0xffffffffu, s.lost) ? warp_sum(slow_squares(b, c, c1)) : warp_sum(s.sum).wide();
+}
 
 struct Coef {
   float coef, pre, mul;
@@ -189,59 +198,78 @@ __device__ __forceinline__ Coef coef_of(double total, float max_norm, float* nor
   return c;
 }
 
+__device__ __forceinline__ uint16_t half_bits(float x) { return __bfloat16_as_ushort(__float2bfloat16(x)); }
+
+// Elements [i0, i1) of a piece whose destination lies differently from its source against 16 bytes: one by one, read
+// again so that a warp's stores are consecutive (the vectors' elements would touch each sector four or eight times).
 template <bool HALF>
-__device__ __forceinline__ void store_scaled(const Piece& p, int lane, const Held& h, const Coef& c) {
-  const bool copy = c.coef == 1.f;  // also keeps a NaN's bits
-  auto scaled = [&](float x) { return x * c.pre * c.mul; };
-  uint8_t* body = p.dst + (p.head << (HALF ? 1 : 2));
-  const bool whole = (reinterpret_cast<uintptr_t>(body) & 15) == 0;
+__device__ __noinline__ void store_apart(const uint8_t* src, uint8_t* dst, int i0, int i1, float pre, float mul,
+                                         bool copy) {
+  constexpr int kBatch = 16;
+  for (int i = i0 + (int)(threadIdx.x & 31); i < i1; i += 32 * kBatch) {
+    uint32_t v[kBatch];
 #pragma unroll
-  for (int q = 0; q < (HALF ? kVecs / 2 : kVecs); ++q) {
-    const int i = lane + 32 * q;
-    uint32_t w[4] = {h.v[q].x, h.v[q].y, h.v[q].z, h.v[q].w};
-    if (!copy) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        w[e] = HALF ? pack_bf16x2(scaled(lo_bf16(w[e])), scaled(hi_bf16(w[e])))
-                    : __float_as_uint(scaled(__uint_as_float(w[e])));
+    for (int k = 0; k < kBatch; ++k) {
+      const int at = min(i + 32 * k, i1 - 1);
+      v[k] = HALF ? (uint32_t) reinterpret_cast<const uint16_t*>(src)[at] : reinterpret_cast<const uint32_t*>(src)[at];
     }
-    if (i >= p.vecs) continue;
-    if (whole) {
-      __stcs(reinterpret_cast<uint4*>(body) + i, make_uint4(w[0], w[1], w[2], w[3]));
-    } else if (HALF) {  // the destination lies differently from the source
-      uint16_t* o = reinterpret_cast<uint16_t*>(body) + 8 * i;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        o[2 * e] = (uint16_t)w[e];
-        o[2 * e + 1] = (uint16_t)(w[e] >> 16);
-      }
-    } else {
-      uint32_t* o = reinterpret_cast<uint32_t*>(body) + 4 * i;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = w[e];
+    for (int k = 0; k < kBatch; ++k) {
+      const int at = i + 32 * k;
+      if (at >= i1) break;
+      if (HALF)
+        reinterpret_cast<uint16_t*>(dst)[at] = copy ? (uint16_t)v[k] : half_bits(__uint_as_float(v[k] << 16) * pre * mul);
+      else
+        reinterpret_cast<uint32_t*>(dst)[at] = copy ? v[k] : __float_as_uint(__uint_as_float(v[k]) * pre * mul);
     }
   }
+}
+
+template <bool HALF, int PART>
+__device__ __forceinline__ void store_scaled(const Piece& p, int lane, const Held& h, const Coef& c) {
+  const bool copy = c.coef == 1.f;  // also keeps a NaN's bits
+  constexpr int kPer = HALF ? 8 : 4, kShift = HALF ? 1 : 2;
+  uint8_t* body = p.dst + (p.head << kShift);
+  const int first = 32 * kVecs * PART;  // vector of the part
+  if ((reinterpret_cast<uintptr_t>(body) & 15) == 0 && c.pre == 1.f) {
+    const int left = p.vecs - lane - first;
+    uint4* o = reinterpret_cast<uint4*>(body) + lane + first;
+#pragma unroll
+    for (int q = 0; q < kVecs; ++q) {
+      uint32_t w[4] = {h.v[q].x, h.v[q].y, h.v[q].z, h.v[q].w};
+      if (!copy) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          w[e] = HALF ? pack_bf16x2(lo_bf16(w[e]) * c.mul, hi_bf16(w[e]) * c.mul)
+                      : __float_as_uint(__uint_as_float(w[e]) * c.mul);
+      }
+      if (32 * q < left) __stcs(o + 32 * q, make_uint4(w[0], w[1], w[2], w[3]));
+    }
+  } else {
+    store_apart<HALF>(p.src, p.dst, p.head + first * kPer, p.head + min(p.vecs, first + 32 * kVecs) * kPer, c.pre, c.mul,
+                      copy);
+  }
+  if (PART != 0) return;
   const int e = edge_index(p, lane);
   if (e < 0) return;
   const float x = __uint_as_float(h.edge);
   if (HALF)
-    reinterpret_cast<uint16_t*>(p.dst)[e] =
-        copy ? (uint16_t)(h.edge >> 16) : __bfloat16_as_ushort(__float2bfloat16(scaled(x)));
+    reinterpret_cast<uint16_t*>(p.dst)[e] = copy ? (uint16_t)(h.edge >> 16) : half_bits(x * c.pre * c.mul);
   else
-    reinterpret_cast<float*>(p.dst)[e] = copy ? x : scaled(x);
+    reinterpret_cast<float*>(p.dst)[e] = copy ? x : x * c.pre * c.mul;
 }
 
+template <int PART>
 __device__ __forceinline__ void store_piece(const Piece& p, int lane, const Held& h, const Coef& c) {
   if (!p.dst || (c.coef == 1.f && p.same)) return;
   if (p.half)
-    store_scaled<true>(p, lane, h, c);
+    store_scaled<true, PART>(p, lane, h, c);
   else
-    store_scaled<false>(p, lane, h, c);
+    store_scaled<false, PART>(p, lane, h, c);
 }
 
-// The CTA's sum, in warp 0; one barrier.
-__device__ __forceinline__ double cta_sum(const Squares& s, double* part) {
-  const double v = s.total();
+// The CTA's sum of the warps', in warp 0; one barrier.
+__device__ __forceinline__ double cta_sum(double v, double* part) {
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
   __syncthreads();
   return threadIdx.x < 32 ? warp_sum(part[threadIdx.x]) : 0.0;
@@ -267,28 +295,27 @@ __global__ void __launch_bounds__(kThreads) clip_sum_kernel(const __grid_constan
   if (c < c1) {
     int i = find_tensor(b, c);
     Piece p = piece_of(b.t[i], c);
-    Held h;
-    load_piece(p, lane, h);
+    Held h0, h1;
+    load_piece<0>(p, lane, h0);
     while (c < c1) {
+      const Piece now = p;
+      load_piece<1>(now, lane, h1);
+      squares.add(now, h0);
       c += kWarps;
-      Piece next_p = p;
-      Held next;
       if (c < c1) {
         while (i + 1 < b.n && c >= b.t[i + 1].chunk_begin) ++i;
-        next_p = piece_of(b.t[i], c);
-        load_piece(next_p, lane, next);
+        p = piece_of(b.t[i], c);
+        load_piece<0>(p, lane, h0);
       }
-      squares.add(p, h);
-      p = next_p;
-      h = next;
+      squares.add(now, h1);
     }
   }
-  const double sum = cta_sum(squares, part);
+  const double sum = cta_sum(warp_total(squares, b, c0 + (int)(threadIdx.x >> 5), c1), part);
   if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
 template <typename Table>
-__global__ void __launch_bounds__(kThreads) clip_scale_kernel(const __grid_constant__ Table b,
+__global__ void __launch_bounds__(32 * kScaleWarps) clip_scale_kernel(const __grid_constant__ Table b,
                                                               const double* __restrict__ partial, int n_partial,
                                                               float max_norm, float* __restrict__ norm_out,
                                                               float* __restrict__ coef_out) {
@@ -299,11 +326,11 @@ __global__ void __launch_bounds__(kThreads) clip_scale_kernel(const __grid_const
   // the tensors were written before the first launch of the call began
   int c = c1 - 1 - (int)(threadIdx.x >> 5), i = 0;
   Piece p;
-  Held h;
+  Held h0, h1;
   if (c >= c0) {
     i = find_tensor(b, c);
     p = piece_of(b.t[i], c);
-    load_piece(p, lane, h);
+    load_piece<0>(p, lane, h0);
   }
   griddep_wait();
   griddep_launch_dependents();
@@ -316,17 +343,16 @@ __global__ void __launch_bounds__(kThreads) clip_scale_kernel(const __grid_const
   __syncthreads();
   const Coef cf = s_coef;
   while (c >= c0) {
-    c -= kWarps;
-    Piece next_p = p;
-    Held next;
+    const Piece now = p;
+    load_piece<1>(now, lane, h1);
+    store_piece<0>(now, lane, h0, cf);
+    c -= kScaleWarps;
     if (c >= c0) {
       while (c < b.t[i].chunk_begin) --i;
-      next_p = piece_of(b.t[i], c);
-      load_piece(next_p, lane, next);
+      p = piece_of(b.t[i], c);
+      load_piece<0>(p, lane, h0);
     }
-    store_piece(p, lane, h, cf);
-    p = next_p;
-    h = next;
+    store_piece<1>(now, lane, h1, cf);
   }
 }
 
@@ -338,24 +364,20 @@ __global__ void __launch_bounds__(kThreads) clip_one_kernel(const __grid_constan
   __shared__ Coef s_coef;
   const int lane = threadIdx.x & 31;
   // pieces go round the CTAs, so that few of them use every SM of the cluster
-  const int c0 = (int)(threadIdx.x >> 5) * kOneCtas + (int)blockIdx.x;
+  const int c = (int)(threadIdx.x >> 5) * kOneCtas + (int)blockIdx.x;
   griddep_wait();
   griddep_launch_dependents();
-  Piece p[kOnePieces];
-  Held h[kOnePieces];
-#pragma unroll
-  for (int k = 0; k < kOnePieces; ++k) {
-    const int c = c0 + k * kOneCtas * kWarps;
-    if (c < b.chunks) {
-      p[k] = piece_of(b.t[find_tensor(b, c)], c);
-      load_piece(p[k], lane, h[k]);
-    }
-  }
+  Piece p;
+  Held h0, h1;
   Squares squares;
-#pragma unroll
-  for (int k = 0; k < kOnePieces; ++k)
-    if (c0 + k * kOneCtas * kWarps < b.chunks) squares.add(p[k], h[k]);
-  double sum = cta_sum(squares, part);
+  if (c < b.chunks) {
+    p = piece_of(b.t[find_tensor(b, c)], c);
+    load_piece<0>(p, lane, h0);
+    load_piece<1>(p, lane, h1);
+    squares.add(p, h0);
+    squares.add(p, h1);
+  }
+  double sum = cta_sum(warp_total(squares, b, c, min(c + 1, b.chunks)), part);
   if (threadIdx.x < kOneCtas) {
     sum = __shfl_sync((1u << kOneCtas) - 1u, sum, 0);
     const uint32_t to = mapa_shared(smem_u32(&all[blockIdx.x]), threadIdx.x);
@@ -368,9 +390,11 @@ __global__ void __launch_bounds__(kThreads) clip_one_kernel(const __grid_constan
     if (threadIdx.x == 0) s_coef = coef_of(v, max_norm, norm_out, coef_out, blockIdx.x == 0);
   }
   __syncthreads();
-#pragma unroll
-  for (int k = 0; k < kOnePieces; ++k)
-    if (c0 + k * kOneCtas * kWarps < b.chunks) store_piece(p[k], lane, h[k], s_coef);
+  if (c < b.chunks) {
+    const Coef cf = s_coef;
+    store_piece<0>(p, lane, h0, cf);
+    store_piece<1>(p, lane, h1, cf);
+  }
 }
 
 template <int N>
@@ -378,6 +402,19 @@ struct Table {
   ClipTensor t[N];
   int n, chunks;
 };
+
+// Lets `kernel` run in clusters of more than eight CTAs, once per device.
+template <typename... KArgs>
+cudaError_t allow_cluster_once(void (*kernel)(KArgs...), std::atomic<unsigned long long>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_acq_rel);
+  return e;
+}
 
 // Runs fn with the batch as a table of the smallest capacity that holds it: the launch copies the whole argument.
 template <typename Fn>
@@ -396,12 +433,16 @@ cudaError_t with_table(const ClipBatch& b, Fn fn) {
     Table<128> t;
     return sized(t);
   }
+  if (b.n <= 448) {
+    Table<448> t;
+    return sized(t);
+  }
   return fn(b);
 }
 
 }  // namespace
 
-bool clip_is_small(const ClipBatch& b) { return b.chunks <= kOneCtas * kWarps * kOnePieces; }
+bool clip_is_small(const ClipBatch& b) { return b.chunks <= kOneCtas * kWarps / 2; }
 
 // A quarter of a CTA's warps at work are enough to keep its loads in flight; more CTAs cost more partial sums.
 int clip_ctas(int chunks, int num_sms) {
@@ -418,13 +459,17 @@ cudaError_t launch_clip_sum(const ClipBatch& b, double* partial, int ctas, cudaS
 cudaError_t launch_clip_scale(const ClipBatch& b, const double* partial, int n_partial, float max_norm, float* norm,
                               float* coef, int ctas, cudaStream_t st) {
   return with_table(b, [&](const auto& t) {
-    return launch_kernel(clip_scale_kernel<std::decay_t<decltype(t)>>, dim3(ctas), dim3(kThreads), 0, st, 1, t,
+    return launch_kernel(clip_scale_kernel<std::decay_t<decltype(t)>>, dim3(ctas), dim3(32 * kScaleWarps), 0, st, 1, t,
                          partial, n_partial, max_norm, norm, coef);
   });
 }
 
 cudaError_t launch_clip_one(const ClipBatch& b, float max_norm, float* norm, float* coef, cudaStream_t st) {
   return with_table(b, [&](const auto& t) {
+    using T = std::decay_t<decltype(t)>;
+    static std::atomic<unsigned long long> done{0};
+    const cudaError_t e = allow_cluster_once(clip_one_kernel<T>, done);
+    if (e != cudaSuccess) return e;
     return launch_kernel(clip_one_kernel<std::decay_t<decltype(t)>>, dim3(kOneCtas), dim3(kThreads), 0, st, kOneCtas,
                          t, max_norm, norm, coef);
   });

@@ -483,7 +483,7 @@ struct ClipTensor {
   int half;         // 1: bf16, 0: fp32
 };
 constexpr int kClipTensors = 1000;  // per launch: the table is a kernel argument, at most 32764 bytes
-constexpr int kClipChunk = 512;     // elements of a piece
+constexpr int kClipChunk = 1024;    // elements of a piece
 
 struct ClipBatch {
   ClipTensor t[kClipTensors];
