@@ -2772,6 +2772,7 @@ int lora_policy_fwd_bwd(const lora_policy_args* a, void* workspace, size_t works
   o.n = at<int>(workspace, pl.n);
   o.u = at<float>(workspace, pl.u);
   o.status = d->status;
+  o.limit_ns = g_wait_limit_ns;
   return rec(launch_policy(o, d->num_sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LORA_OK : LORA_ECUDA);
 }
 
@@ -2816,6 +2817,7 @@ int lora_pref_fwd_bwd(const lora_pref_args* a, void* workspace, size_t workspace
   o.n = at<int>(workspace, pl.n);
   o.u = at<float>(workspace, pl.u);
   o.status = d->status;
+  o.limit_ns = g_wait_limit_ns;
   return rec(launch_pref(o, d->num_sms, static_cast<cudaStream_t>(stream)) == cudaSuccess ? LORA_OK : LORA_ECUDA);
 }
 

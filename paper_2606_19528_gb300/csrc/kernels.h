@@ -470,6 +470,7 @@ struct Objective {
   int* n;             // [groups]: trainable tokens
   float* u;           // [T]: the tokens' weights, but for the factor 1 / (trainable tokens of the batch)
   int* status;
+  long long limit_ns;
 };
 cudaError_t launch_policy(const Objective& o, int num_sms, cudaStream_t stream);
 cudaError_t launch_pref(const Objective& o, int num_sms, cudaStream_t stream);

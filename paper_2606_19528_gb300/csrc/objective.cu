@@ -2,9 +2,11 @@
 //   policy_kernel  clipped policy loss with a KL term, one cluster of 1 or 8 CTAs per sequence
 //   pref_kernel    loss of a chosen against a rejected sequence, one cluster per pair
 //   rows_kernel    the loss's sum, the tokens' weights w_t = d loss / d nll_t, and dh_t = w_t * d nll_t / d h_t
-// The first launch reads a few bytes per token; the second streams two rows of d bf16 per token and is bound by
-// memory.  It needs the first one's sums (a weight depends on its whole sequence or batch), but starts beside it: its
-// first rows are on their way when the sums arrive.
+// The first launch reads a few bytes per token and is a chain of latencies (about 4.5 us with the launches); the
+// second streams two rows of d bf16 per trainable token, one per masked token, and is bound by memory: 58 us for the
+// 352 MB of 49152 tokens of 2048, a quarter of them masked, 0.9 of the copy rate.  It needs the first one's sums (a
+// weight depends on its whole sequence or batch), but starts beside it: its first rows are on their way when the sums
+// arrive.
 //
 // Sums over tokens are held as pairs of fp32 (48 bits).
 #include <math.h>
@@ -327,72 +329,113 @@ __device__ __forceinline__ long long count_tokens(const Objective& o) {
   return n;
 }
 
-// Block 0 finishes the loss.  The others' warps take parts of rows: four 16-byte vectors a lane, the next part's
-// loads issued before this one is written, the weight of the one after that on its way.
-constexpr int kVecs = 4;
+// Block 0 finishes the loss.  The others' warps take parts of rows, each through a ring of bulk copies of its own:
+// the copies need no registers, so that 192 KB per SM are on their way while the first launch still runs.  16384
+// tokens of 3072 for 32 pairs take 29.1 us as four blocks of 8 warps by 3 slots per SM, 30.1 as two by 6, 28.7 as six
+// by 2; 49152 tokens of 2048 take 63.1, 63.7 and 64.6; 4096 of 3072 take 8.6, 9.4 and 9.0.  Loads one part ahead
+// into registers, four blocks per SM: 31.3, 63 and 9.4.
+constexpr int kVecs = 4;               // 16-byte vectors of a lane
+constexpr int kPartVecs = 32 * kVecs;  // of a part
+constexpr int kSlots = 3;              // parts of a warp
+constexpr int kRowCtas = 4;            // per SM
+constexpr uint32_t kPartBytes = 16u * kPartVecs;
+constexpr uint32_t kRowsSmem = kWarps * kSlots * (kPartBytes + 8u);
+constexpr long long kDrainNs = 200000000;
 
-__global__ void __launch_bounds__(kThreads) rows_kernel(const __grid_constant__ Objective o) {
+__global__ void __launch_bounds__(kThreads, kRowCtas) rows_kernel(const __grid_constant__ Objective o) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ volatile int s_abort;
   if (blockIdx.x == 0) {
     griddep_wait();
     griddep_launch_dependents();
     finish(o);
     return;
   }
-  const int lane = threadIdx.x & 31, vecs = o.dh ? o.d / 8 : 0;
-  const int parts = o.dh ? (vecs + 32 * kVecs - 1) / (32 * kVecs) : 1;
-  const int warps = ((int)gridDim.x - 1) * kWarps, w0 = ((int)blockIdx.x - 1) * kWarps + (int)(threadIdx.x >> 5);
-  const int dt = warps / parts, dp = warps % parts;
-  struct At {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const WaitCtl wait{o.status, o.limit_ns};
+  const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * kSlots) * kPartBytes;
+  const uint32_t bars = smem_u32(smem) + (uint32_t)(kWarps * kSlots) * kPartBytes + (uint32_t)(warp * kSlots) * 8u;
+  if (o.dh && lane < kSlots) mbar_init(bars + 8 * lane, 1);
+  if (threadIdx.x == 0) s_abort = 0;
+  fence_mbar_init();
+  __syncthreads();
+
+  const int vecs = o.dh ? o.d / 8 : 0, parts = o.dh ? (vecs + kPartVecs - 1) / kPartVecs : 1;
+  const long long warps = ((long long)gridDim.x - 1) * kWarps, w0 = ((long long)blockIdx.x - 1) * kWarps + warp;
+  // The warp's i-th part; lane l holds those with i % 32 == l, of this round of 32 and the next.
+  struct Part {
     int t, part;
+    bool copied;
+    float u;
   };
-  auto next = [&](At a) {
-    a.t += dt;
-    a.part += dp;
-    if (a.part >= parts) {
-      a.part -= parts;
-      ++a.t;
-    }
-    return a;
+  auto place = [&](long long i) {
+    const long long id = w0 + i * warps, t = id / parts;
+    return Part{t < o.T ? (int)t : o.T, (int)(id - t * parts), false, 0.f};
   };
-  uint4 q[kVecs];
-  auto fetch = [&](At a, bool wanted) {
-    const uint4* src = reinterpret_cast<const uint4*>(o.dh_nll + (long long)a.t * o.d);
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) {
-      const int v = (a.part * kVecs + k) * 32 + lane;
-      q[k] = wanted && v < vecs ? __ldcs(src + v) : make_uint4(0u, 0u, 0u, 0u);
-    }
+  auto weigh = [&](Part& p) { p.u = p.t < o.T ? o.u[p.t] : 0.f; };
+  auto copy = [&](const Part& p, int slot) {
+    const int n = min(kPartVecs, vecs - p.part * kPartVecs);
+    mbar_arrive_expect_tx(bars + 8 * slot, 16u * n);
+    bulk_load(ring + slot * kPartBytes, o.dh_nll + (long long)p.t * o.d + (long long)p.part * (8 * kPartVecs), 16u * n,
+              bars + 8 * slot);
   };
-  At a{w0 / parts, w0 % parts};
+  Part cur = place(lane);
   // the mask and the rows were written before the first launch of the call began
-  fetch(a, o.dh && a.t < o.T && (!o.mask || o.mask[a.t]));
+  if (o.dh && lane < kSlots && cur.t < o.T && (!o.mask || o.mask[cur.t])) {
+    copy(cur, lane);
+    cur.copied = true;
+  }
+  uint32_t pending = __ballot_sync(0xffffffffu, cur.copied);  // bit s: a copy is on its way to slot s
+  uint32_t phases = 0;                                         // bit s: the parity of its wait
   griddep_wait();
   griddep_launch_dependents();
-  At b = next(a);
-  float ua = a.t < o.T ? o.u[a.t] : 0.f, ub = b.t < o.T ? o.u[b.t] : 0.f;
+  weigh(cur);
   float inv = 1.f;
   if (o.reduction == LORA_MEAN_TOKENS) {
     const long long n = count_tokens(o);
     inv = n ? 1.f / (float)n : 1.f;
   }
-  while (a.t < o.T) {
-    const float w = ua * inv;
-    uint4 r[kVecs];
+  if (o.dh && lane >= kSlots) cur.copied = cur.u != 0.f;  // also a NaN; a row of weight zero is not read
+  int slot = 0;
+  bool more = true;
+  for (long long base = 0; more; base += 32) {
+    Part nxt = place(base + 32 + lane);
+    weigh(nxt);
+    if (o.dh) nxt.copied = nxt.u != 0.f;
+    for (int k = 0; k < 32; ++k) {
+      const int t = __shfl_sync(0xffffffffu, cur.t, k), part = __shfl_sync(0xffffffffu, cur.part, k);
+      const float u = __shfl_sync(0xffffffffu, cur.u, k), w = u * inv;
+      const bool copied = __shfl_sync(0xffffffffu, (int)cur.copied, k);
+      more = t < o.T;
+      if (!more) break;
+      if (o.token_weight && part == 0 && lane == 0) o.token_weight[t] = w;
+      if (!o.dh) continue;
+      uint4 r[kVecs] = {};
+      if (copied) {
+        more = __all_sync(0xffffffffu, mbar_wait(bars + 8 * slot, (phases >> slot) & 1u, wait, &s_abort));
+        if (!more) break;
+        phases ^= 1u << slot;
+        pending &= ~(1u << slot);
 #pragma unroll
-    for (int k = 0; k < kVecs; ++k) r[k] = q[k];
-    fetch(b, o.dh && ub != 0.f);  // also a NaN
-    const At c = next(b);
-    const float uc = c.t < o.T ? o.u[c.t] : 0.f;
-    if (o.token_weight && a.part == 0 && lane == 0) o.token_weight[a.t] = w;
-    if (o.dh) {
-      uint4* dst = reinterpret_cast<uint4*>(o.dh + (long long)a.t * o.d);
+        for (int q = 0; q < kVecs; ++q)
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(r[q].x), "=r"(r[q].y), "=r"(r[q].z), "=r"(r[q].w)
+                       : "r"(ring + slot * kPartBytes + 16u * (uint32_t)(32 * q + lane))
+                       : "memory");
+        __syncwarp();
+      }
+      // the part kSlots on takes the slot
+      const bool refill = lane == ((k + kSlots) & 31) && (k + kSlots < 32 ? cur : nxt).copied;
+      if (refill) copy(k + kSlots < 32 ? cur : nxt, slot);
+      if (__any_sync(0xffffffffu, refill)) pending |= 1u << slot;
+      uint4* dst = reinterpret_cast<uint4*>(o.dh + (long long)t * o.d);
 #pragma unroll
-      for (int k = 0; k < kVecs; ++k) {
-        const int v = (a.part * kVecs + k) * 32 + lane;
+      for (int q = 0; q < kVecs; ++q) {
+        const int v = (part * kVecs + q) * 32 + lane;
         if (v >= vecs) continue;
         uint4 out = make_uint4(0u, 0u, 0u, 0u);
-        if (ua != 0.f) {  // a row of weight zero is zero whatever it holds
-          const uint32_t in[4] = {r[k].x, r[k].y, r[k].z, r[k].w};
+        if (u != 0.f) {  // a row of weight zero is zero whatever it holds
+          const uint32_t in[4] = {r[q].x, r[q].y, r[q].z, r[q].w};
           uint32_t x[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -401,12 +444,13 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(const __grid_constant__ 
         }
         __stcs(dst + v, out);
       }
+      if (++slot == kSlots) slot = 0;
     }
-    a = b;
-    b = c;
-    ua = ub;
-    ub = uc;
+    if (more) cur = nxt;
   }
+  // not empty only after a wait that gave up: no copy outlives the block's shared memory (bounded)
+  for (int s = 0; s < kSlots; ++s)
+    if ((pending >> s) & 1u) mbar_wait_drain(bars + 8 * s, (phases >> s) & 1u, kDrainNs);
 }
 
 // Eight CTAs share a group where groups hold over a token per thread on average (the longest of an uneven batch
@@ -418,10 +462,13 @@ int cluster_for(const Objective& o, int num_sms) {
 cudaError_t launch_rows(const Objective& o, int num_sms, cudaStream_t st) {
   int ctas = 0;
   if (o.dh || o.token_weight) {
-    const long long parts = o.dh ? (o.d / 8 + 32 * kVecs - 1) / (32 * kVecs) : 1;
-    ctas = (int)std::min<long long>((o.T * parts + kWarps - 1) / kWarps, 4 * num_sms);
+    const long long parts = o.dh ? (o.d / 8 + kPartVecs - 1) / kPartVecs : 1;
+    ctas = (int)std::min<long long>((o.T * parts + kWarps - 1) / kWarps, kRowCtas * num_sms - 1);  // and block 0
   }
-  return launch_kernel(rows_kernel, dim3(1 + ctas), dim3(kThreads), 0, st, 1, o);
+  static std::atomic<unsigned long long> done{0};
+  const cudaError_t e = set_smem_once(rows_kernel, kRowsSmem, done);
+  if (e != cudaSuccess) return e;
+  return launch_kernel(rows_kernel, dim3(1 + ctas), dim3(kThreads), o.dh ? kRowsSmem : 0, st, 1, o);
 }
 
 }  // namespace
