@@ -54,8 +54,8 @@ __device__ __forceinline__ int su_image_at(int r, int tok, int col, int term) {
 
 // One block per (projection, adapter row j): su[t, j] = scale * x_t . A_j for up to TT tokens.
 constexpr int kSuThreads = 256;
-template <int TT>
-__global__ void __launch_bounds__(kSuThreads) decode_su_kernel(const __grid_constant__ DecodeBatch b) {
+template <int TT, typename Table>
+__global__ void __launch_bounds__(kSuThreads) decode_su_kernel(const __grid_constant__ Table b) {
   griddep_wait();
   griddep_launch_dependents();
   int i = 0;
@@ -124,8 +124,8 @@ struct Step {
 // two to four steps ahead takes the registers of as many warps and is slower.  A lane's word of 8 codes makes the fragments of two MMAs, whose k index is
 // then a permutation of the columns; the activation's fragments share it: 16 consecutive bytes of token g, which come
 // through L1.
-template <int NT>  // tokens / 8
-__global__ void __launch_bounds__(kMostThreads) decode_kernel(const __grid_constant__ DecodeBatch b) {
+template <int NT, typename Table>  // tokens / 8
+__global__ void __launch_bounds__(kMostThreads) decode_kernel(const __grid_constant__ Table b) {
   constexpr int kChains = NT == 1 ? 2 : 1;  // of dependent MMAs: two at least
   const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   if (!b.after_su) griddep_wait();  // otherwise the launch before is this call's, and began after its inputs were there
@@ -248,17 +248,23 @@ cudaError_t launch_narrow(DecodeBatch& b, int most, int num_sms, cudaStream_t st
       least = cost;
     }
   }
-  return most <= 8 ? launch_kernel(decode_kernel<1>, dim3(tiles), dim3(32 * warps), 0, st, 1, b)
-                   : launch_kernel(decode_kernel<2>, dim3(tiles), dim3(32 * warps), 0, st, 1, b);
+  return with_table(b, [&](const auto& t) {
+    using Table = std::decay_t<decltype(t)>;
+    return launch_kernel(most <= 8 ? decode_kernel<1, Table> : decode_kernel<2, Table>, dim3(tiles), dim3(32 * warps), 0,
+                         st, 1, t);
+  });
 }
 
 cudaError_t launch_su(const DecodeBatch& b, int most, cudaStream_t st) {
-  const auto su = most == 1   ? decode_su_kernel<1>
-                  : most <= 2 ? decode_su_kernel<2>
-                  : most <= 4 ? decode_su_kernel<4>
-                  : most <= 8 ? decode_su_kernel<8>
-                              : decode_su_kernel<16>;
-  return launch_kernel(su, dim3(b.rows), dim3(kSuThreads), 0, st, 1, b);
+  return with_table(b, [&](const auto& t) {
+    using Table = std::decay_t<decltype(t)>;
+    const auto su = most == 1   ? decode_su_kernel<1, Table>
+                    : most <= 2 ? decode_su_kernel<2, Table>
+                    : most <= 4 ? decode_su_kernel<4, Table>
+                    : most <= 8 ? decode_su_kernel<8, Table>
+                                : decode_su_kernel<16, Table>;
+    return launch_kernel(su, dim3(t.rows), dim3(kSuThreads), 0, st, 1, t);
+  });
 }
 
 // Which second launch a group of projections takes, by their times as measured (us): 16-row blocks read their bytes at
@@ -293,7 +299,7 @@ void set_decode_su(DecodeProj& p, void* at) {
 }
 
 cudaError_t launch_decode(DecodeBatch& b, int num_sms, cudaStream_t st) {
-  b.rows = 0;
+  b.rows = b.after_su = 0;
   int most = 1;
   for (int i = 0; i < b.n; ++i) {
     b.p[i].row_begin = b.rows;
@@ -306,7 +312,7 @@ cudaError_t launch_decode(DecodeBatch& b, int num_sms, cudaStream_t st) {
   }
   // projections of many rows: one launch for those that read one activation (gate and up); one for all the others
   DecodeBatch rest, same;
-  rest.n = 0;
+  rest.n = rest.rows = same.rows = 0;
   rest.after_su = same.after_su = b.rows > 0;
   rest.status = same.status = b.status;
   rest.limit_ns = same.limit_ns = b.limit_ns;

@@ -60,12 +60,19 @@ __device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+template <int CAP>
+struct CodeMaps {
+  CUtensorMap codes[CAP];
+};
+
 struct Wide {
   int tiles, stages;
   int held;  // 1: the whole activation stays in shared memory, behind the stages; 0: a stage carries its columns
 };
 
-__global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_constant__ DecodeBatch b,
+template <typename Table>
+__global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_constant__ Table b,
+                                                                  const __grid_constant__ CodeMaps<Table::kCap> maps,
                                                                   const __grid_constant__ CUtensorMap x_map,
                                                                   const __grid_constant__ Wide wide) {
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -134,7 +141,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
           const uint32_t at = ring + s * stage_bytes, bar = full + 8 * s;
           const bool with_x = !wide.held || first;  // the held activation comes with the first tile's codes
           mbar_arrive_expect_tx(bar, kCodeBytes + (with_x ? kXBytes : 0u));
-          tma_load_2d(at, &b.codes[proj], bar, c * (kPanel / 2), n0);
+          tma_load_2d(at, &maps.codes[proj], bar, c * (kPanel / 2), n0);
           if (with_x)
             for (int i = 0; i < kPanel / 64; ++i)
               tma_load_2d((wide.held ? held + c * kXBytes : at + kCodeBytes) + i * kXBlock, &x_map, bar,
@@ -393,18 +400,13 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
 }  // namespace
 
 cudaError_t launch_decode_wide(DecodeBatch& b, int num_sms, cudaStream_t st) {
-  static std::atomic<unsigned long long> done{0};
-  const cudaError_t e = set_smem_once(decode_wide_kernel, kMostSmem, done);
-  if (e != cudaSuccess) return e;
   const DecodeProj& p0 = b.p[0];
   const int panels = (p0.K + kPanel - 1) / kPanel;
   Wide w;
   w.tiles = 0;
   for (int i = 0; i < b.n; ++i) {
-    DecodeProj& p = b.p[i];
-    p.tile_begin = w.tiles;
-    w.tiles += (p.N + kRows - 1) / kRows;
-    if (!make_bytes_map(&b.codes[i], p.codes, p.K / 2, p.N, kPanel / 2, kRows)) return cudaErrorInvalidValue;
+    b.p[i].tile_begin = w.tiles;
+    w.tiles += (b.p[i].N + kRows - 1) / kRows;
   }
   CUtensorMap x_map;
   if (!make_bf16_map(&x_map, p0.x, p0.K, p0.T, 64, kTok)) return cudaErrorInvalidValue;
@@ -414,7 +416,18 @@ cudaError_t launch_decode_wide(DecodeBatch& b, int num_sms, cudaStream_t st) {
   const int stage = kCodeBytes + (w.held ? 0 : kXBytes);
   w.stages = std::min(kMaxStages, (room - (w.held ? all : 0)) / stage) / kGroups * kGroups;
   const size_t smem = (size_t)w.stages * stage + (w.held ? all : 0) + sizeof(Ctl);
-  return launch_kernel(decode_wide_kernel, dim3(std::min(w.tiles, num_sms)), dim3(kThreads), smem, st, 1, b, x_map, w);
+  return with_table(b, [&](const auto& t) {
+    using Table = std::decay_t<decltype(t)>;
+    CodeMaps<Table::kCap> maps;
+    for (int i = 0; i < t.n; ++i)
+      if (!make_bytes_map(&maps.codes[i], t.p[i].codes, t.p[i].K / 2, t.p[i].N, kPanel / 2, kRows))
+        return cudaErrorInvalidValue;
+    static std::atomic<unsigned long long> done{0};
+    const cudaError_t e = set_smem_once(decode_wide_kernel<Table>, kMostSmem, done);
+    if (e != cudaSuccess) return e;
+    return launch_kernel(decode_wide_kernel<Table>, dim3(std::min(w.tiles, num_sms)), dim3(kThreads), smem, st, 1, t, maps,
+                         x_map, w);
+  });
 }
 
 }  // namespace lora

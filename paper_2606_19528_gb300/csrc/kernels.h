@@ -412,14 +412,31 @@ struct DecodeProj {
   int row_begin;   // first of its adapter rows in the first launch's list
 };
 
-struct DecodeBatch {
-  CUtensorMap codes[kDecodeMaxProjs];
-  DecodeProj p[kDecodeMaxProjs];
+// A kernel's argument: the launch copies all of it, so that calls of few projections have a small one (below).
+template <int CAP>
+struct DecodeTable {
+  static constexpr int kCap = CAP;
+  DecodeProj p[CAP];
   int n, rows;
   int after_su;  // the launch follows one that computes su
   int* status;
   long long limit_ns;
 };
+using DecodeBatch = DecodeTable<kDecodeMaxProjs>;
+
+// fn(table) with the smallest table that holds the batch.
+template <typename Fn>
+cudaError_t with_table(const DecodeBatch& b, Fn fn) {
+  if (b.n > 8) return fn(b);
+  DecodeTable<8> t;
+  for (int i = 0; i < b.n; ++i) t.p[i] = b.p[i];
+  t.n = b.n;
+  t.rows = b.rows;
+  t.after_su = b.after_su;
+  t.status = b.status;
+  t.limit_ns = b.limit_ns;
+  return fn(t);
+}
 
 // su times 2^-40 (like the weights, dq40_word) is held as three bf16 terms, all 24 bits of its fp32 value, zeros
 // behind column r:
