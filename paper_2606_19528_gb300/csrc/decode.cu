@@ -1,16 +1,20 @@
 // Forward of adapted projections with 4-bit weights for 1 to 16 tokens:
-//   decode_su_kernel  su = scale * x A^T, one block per adapter row
-//   decode_kernel     y  = x W^T + su B^T, W[n, k] = bf16(s q + b) from its 4-bit codes
+//   decode_su_kernel    su = scale * x A^T, one block per adapter row
+//   decode_kernel       y  = x W^T + su B^T, W[n, k] = bf16(s q + b) from its 4-bit codes, 16 rows of W per block
+//   decode_wide_kernel  the same, for many rows (decode_wide.cu)
 //
 // With so few tokens every weight is used once or a handful of times, so the call is bound by reading 9/16 byte per
-// weight, and next by the instructions that dequantize it.  The products go through mma.sync m16n8k16, whose 8
-// columns are the tokens: an accumulation on the FMA units would take two conversions and 2 T FMAs per pair of
-// weights more, and the tcgen05 path wants its operands in shared memory, where the round trip of the dequantized
-// weights alone costs more than the products of 16 tokens.
+// weight, and next by the instructions that dequantize it; small calls are bound by a chain of latencies (launch,
+// codes, products, the warps' sums) and by the host's launches.  Dequantizing takes 9 instructions per 8 codes
+// (dq40_word); the sums are scaled back by 2^40.  The products go through mma.sync m16n8k16, whose 8 columns are the
+// tokens: on the FMA units a pair of weights would take two conversions and 2 T FMAs more.  An MMA holds a sub-core's
+// tensor unit for 24 clocks, which bounds 9 to 16 tokens; the wide launch goes past that.
 //
-// Dequantizing takes 9 instructions per 8 codes (dq40_word); the sums are scaled back by 2^40.
+// su enters the same MMAs as three bf16 terms, which hold all 24 bits of its fp32 value: rounding it to bf16 would
+// add an error of 2^-9 of the adapter's part.
 //
-// su enters the same MMAs as three bf16 terms, which hold all 24 bits of its fp32 value.
+// One token, q, k and v of 3072 columns (N 3072, 1024, 1024; r 16), 9.3 MB: 5.4 us, 1.7 TB/s; 8192 x 3072: 7.2 us, 2
+// TB/s; five tokens, two of 2048 x 11008, r 64, 29 MB: 10.8 us, 2.7 TB/s.
 #include <algorithm>
 
 #include "common.cuh"
@@ -121,10 +125,13 @@ struct Step {
 
 // One block per 16 output rows, its warps sharing out the columns: warp i has every warps-th chunk of 128 from i on, and
 // every warps-th 16 of the adapter's columns.  A step's weights are loaded while the one before is computed; loading
-// two to four steps ahead takes the registers of as many warps and is slower.  A lane's word of 8 codes makes the fragments of two MMAs, whose k index is
-// then a permutation of the columns; the activation's fragments share it: 16 consecutive bytes of token g, which come
-// through L1.
-template <int NT, typename Table>  // tokens / 8
+// two to four steps ahead takes the registers of as many warps and is slower.  A lane's word of 8 codes makes the
+// fragments of two MMAs, whose k index is then a permutation of the columns; the activation's fragments share it: 16
+// consecutive bytes of token g, which come through L1.
+//
+// OWN: each block computes su of its projection beside y, from all of A, in the same loop: 16 adapter rows are one more
+// tile, whose fragments come from A as they lie; no launch goes before.
+template <int NT, bool OWN, typename Table>  // tokens / 8
 __global__ void __launch_bounds__(kMostThreads) decode_kernel(const __grid_constant__ Table b) {
   constexpr int kChains = NT == 1 ? 2 : 1;  // of dependent MMAs: two at least
   const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -170,7 +177,12 @@ __global__ void __launch_bounds__(kMostThreads) decode_kernel(const __grid_const
   uint32_t adapter[4];
   load_adapter(16 * warp, adapter);
 
-  float acc[kChains][NT][4] = {};
+  float acc[kChains][NT][4] = {}, sacc[OWN ? NT : 1][4] = {};
+  const uint4 *a0 = nullptr, *a1 = nullptr;
+  if (OWN && r) {
+    a0 = reinterpret_cast<const uint4*>(p.A + (long long)min(g, r - 1) * K + 32 * t);
+    a1 = reinterpret_cast<const uint4*>(p.A + (long long)min(g + 8, r - 1) * K + 32 * t);
+  }
   const uint4* x4[NT];  // columns past T are dropped: whatever token their fragments hold
 #pragma unroll
   for (int m = 0; m < NT; ++m)
@@ -186,7 +198,22 @@ __global__ void __launch_bounds__(kMostThreads) decode_kernel(const __grid_const
     for (int m = 0; m < NT; ++m)
 #pragma unroll
       for (int q = 0; q < 4; ++q) xv[m][q] = in ? __ldg(x4[m] + c * (kChunk / 8) + q) : make_uint4(0u, 0u, 0u, 0u);
+    uint4 av[OWN ? 4 : 1][2];
+    if (OWN && r)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        av[q][0] = in ? __ldg(a0 + c * (kChunk / 8) + q) : make_uint4(0u, 0u, 0u, 0u);
+        av[q][1] = in && r > 8 ? __ldg(a1 + c * (kChunk / 8) + q) : make_uint4(0u, 0u, 0u, 0u);
+      }
     fetch(s, c + warps);
+    if (OWN && r)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int m = 0; m < NT; ++m) {
+          mma_bf16(sacc[m], av[q][0].x, av[q][1].x, av[q][0].y, av[q][1].y, xv[m][q].x, xv[m][q].y);
+          mma_bf16(sacc[m], av[q][0].z, av[q][1].z, av[q][0].w, av[q][1].w, xv[m][q].z, xv[m][q].w);
+        }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       uint32_t a[2][4];
@@ -200,7 +227,7 @@ __global__ void __launch_bounds__(kMostThreads) decode_kernel(const __grid_const
     }
   }
   if (b.after_su) griddep_wait();  // su
-  for (int j0 = 16 * warp; j0 < r; j0 += 16 * warps) {
+  for (int j0 = OWN ? r : 16 * warp; j0 < r; j0 += 16 * warps) {
     if (j0 != 16 * warp) load_adapter(j0, adapter);
     __syncwarp();
 #pragma unroll
@@ -219,16 +246,39 @@ __global__ void __launch_bounds__(kMostThreads) decode_kernel(const __grid_const
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       red[warp][8 * m + 2 * t + (e & 1)][g + 8 * (e >> 1)] = kChains == 2 ? acc[0][m][e] + acc[kChains - 1][m][e] : acc[0][m][e];
+  __shared__ float su_red[OWN ? kMostThreads / 32 : 1][NT * 8][kRedPitch], s_su[NT * 8][16], s_b[kTileN][17];
+  if constexpr (OWN) {
+#pragma unroll
+    for (int m = 0; m < NT; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) su_red[warp][8 * m + 2 * t + (e & 1)][g + 8 * (e >> 1)] = sacc[m][e];
+    if (warp == 0)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s_b[g + 8 * (e & 1)][2 * t + 8 * (e >> 1)] = lo_bf16(adapter[e]);
+        s_b[g + 8 * (e & 1)][2 * t + 8 * (e >> 1) + 1] = hi_bf16(adapter[e]);
+      }
+    __syncthreads();
+    for (int o = threadIdx.x; o < 16 * T; o += blockDim.x) {
+      float v = 0.f;
+      for (int w = 0; w < warps; ++w) v += su_red[w][o / 16][o % 16];
+      s_su[o / 16][o % 16] = o % 16 < r ? v * p.scale : 0.f;
+    }
+  }
   __syncthreads();
   for (int o = threadIdx.x; o < kTileN * T; o += blockDim.x) {
     const int tok = o / kTileN, row = o % kTileN, n = n0 + row;
     float v = 0.f;
     for (int w = 0; w < warps; ++w) v += red[w][tok][row];
-    if (n < p.N) p.y[(long long)tok * p.N + n] = __float2bfloat16(v * 0x1p40f);
+    v *= 0x1p40f;
+    if (OWN && r)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v = fmaf(s_su[tok][j], s_b[row][j], v);
+    if (n < p.N) p.y[(long long)tok * p.N + n] = __float2bfloat16(v);
   }
 }
 
-cudaError_t launch_narrow(DecodeBatch& b, int most, int num_sms, cudaStream_t st) {
+cudaError_t launch_narrow(DecodeBatch& b, int most, bool own, int num_sms, cudaStream_t st) {
   int tiles = 0, chunks = 1;
   for (int i = 0; i < b.n; ++i) {
     b.p[i].tile_begin = tiles;
@@ -250,8 +300,10 @@ cudaError_t launch_narrow(DecodeBatch& b, int most, int num_sms, cudaStream_t st
   }
   return with_table(b, [&](const auto& t) {
     using Table = std::decay_t<decltype(t)>;
-    return launch_kernel(most <= 8 ? decode_kernel<1, Table> : decode_kernel<2, Table>, dim3(tiles), dim3(32 * warps), 0,
-                         st, 1, t);
+    const auto kernel = own         ? decode_kernel<1, true, Table>
+                        : most <= 8 ? decode_kernel<1, false, Table>
+                                    : decode_kernel<2, false, Table>;
+    return launch_kernel(kernel, dim3(tiles), dim3(32 * warps), 0, st, 1, t);
   });
 }
 
@@ -287,6 +339,25 @@ bool wide_pays(const DecodeBatch& b, int num_sms) {
   return wide < blocks;
 }
 
+// Whether the blocks compute su themselves, with all of A read by each of them, against a launch before theirs: a
+// launch less costs the host 1.9 us less, which bounds calls this small, and the reading again costs the GPU next to
+// nothing up to 4.5 MB of it by one block per SM.  (One token, the GPU alone, then calls in a row; with and without the
+// launch before: 256 x 256, r 8, 2.9 and 2.2 us, 5.9 and 4.0; 1024 x 2048, r 16, 4.2 MB, 3.4 and 3.5, 5.9 and 4.0;
+// 2048 x 2048, r 8, 4.2 MB, 3.5 and 3.8, 5.9 and 4.1; 3072 x 1024, r 16, 6.3 MB, 4.1 and 5.3, 5.9 and 5.6; 3072 x
+// 3072, r 16, 18.9 MB, 4.5 and 7.9, 6.1 and 8.1; 64 x 29768, r 16, 3.8 MB by 1861 blocks, 3.5 and 4.4, with eight tokens
+// 3.7 and 6.3.)  More tokens or adapter rows would not fit the registers.
+bool own_pays(const DecodeBatch& b, int num_sms) {
+  int tiles = 0;
+  double again = 0.0;
+  for (int i = 0; i < b.n; ++i) {
+    const DecodeProj& p = b.p[i];
+    if (p.r > 16 || p.T > 8) return false;
+    tiles += (p.N + kTileN - 1) / kTileN;
+    again += (double)((p.N + kTileN - 1) / kTileN) * p.r * p.K * 2e-6;
+  }
+  return tiles <= num_sms && again <= 4.5;
+}
+
 }  // namespace
 
 size_t decode_su_bytes(int64_t T, int64_t r) {
@@ -299,42 +370,53 @@ void set_decode_su(DecodeProj& p, void* at) {
 }
 
 cudaError_t launch_decode(DecodeBatch& b, int num_sms, cudaStream_t st) {
-  b.rows = b.after_su = 0;
-  int most = 1;
+  // projections of many rows: one launch for those that read one activation (gate and up); one for all the others
+  DecodeBatch rest, same;
+  rest.n = rest.rows = same.rows = b.rows = b.after_su = 0;
+  rest.status = same.status = b.status;
+  rest.limit_ns = same.limit_ns = b.limit_ns;
+  int group[kDecodeMaxProjs], most = 1, most_rest = 1;  // the first projection of a wide launch's, or -1
   for (int i = 0; i < b.n; ++i) {
     b.p[i].row_begin = b.rows;
     b.rows += b.p[i].r;
     most = std::max(most, b.p[i].T);
+    group[i] = i;
+    for (int j = 0; j < i && group[i] == i; ++j)
+      if (b.p[j].x == b.p[i].x && b.p[j].T == b.p[i].T && b.p[j].K == b.p[i].K) group[i] = j;
   }
-  if (b.rows) {
+  auto gather = [&](int first) {
+    same.n = 0;
+    for (int i = first; i < b.n; ++i)
+      if (group[i] == first) same.p[same.n++] = b.p[i];
+  };
+  bool wide[kDecodeMaxProjs], any_wide = false;
+  for (int i = 0; i < b.n; ++i) {
+    if (group[i] != i) {
+      wide[i] = wide[group[i]];
+    } else {
+      gather(i);
+      wide[i] = wide_pays(same, num_sms);
+    }
+    if (wide[i]) {
+      any_wide = true;
+    } else {
+      rest.p[rest.n++] = b.p[i];
+      most_rest = std::max(most_rest, b.p[i].T);
+    }
+  }
+  const bool own = b.rows && !any_wide && own_pays(rest, num_sms);
+  rest.after_su = same.after_su = b.rows > 0 && !own;
+  if (rest.after_su) {
     const cudaError_t e = launch_su(b, most, st);
     if (e != cudaSuccess) return e;
   }
-  // projections of many rows: one launch for those that read one activation (gate and up); one for all the others
-  DecodeBatch rest, same;
-  rest.n = rest.rows = same.rows = 0;
-  rest.after_su = same.after_su = b.rows > 0;
-  rest.status = same.status = b.status;
-  rest.limit_ns = same.limit_ns = b.limit_ns;
-  bool taken[kDecodeMaxProjs] = {};
-  most = 1;
-  for (int i = 0; i < b.n; ++i) {
-    if (taken[i]) continue;
-    same.n = 0;
-    for (int j = i; j < b.n; ++j) {
-      if (taken[j] || b.p[j].x != b.p[i].x || b.p[j].T != b.p[i].T || b.p[j].K != b.p[i].K) continue;
-      taken[j] = true;
-      same.p[same.n++] = b.p[j];
-    }
-    if (wide_pays(same, num_sms)) {
-      const cudaError_t e = launch_decode_wide(same, num_sms, st);
-      if (e != cudaSuccess) return e;
-    } else {
-      for (int j = 0; j < same.n; ++j) rest.p[rest.n++] = same.p[j];
-      most = std::max(most, b.p[i].T);
-    }
+  for (int i = 0; any_wide && i < b.n; ++i) {
+    if (!wide[i] || group[i] != i) continue;
+    gather(i);
+    const cudaError_t e = launch_decode_wide(same, num_sms, st);
+    if (e != cudaSuccess) return e;
   }
-  return rest.n ? launch_narrow(rest, most, num_sms, st) : cudaSuccess;
+  return rest.n ? launch_narrow(rest, most_rest, own, num_sms, st) : cudaSuccess;
 }
 
 }  // namespace lora
