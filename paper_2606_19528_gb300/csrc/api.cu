@@ -2200,6 +2200,10 @@ int clip_batches(const lora_grad* grads, int n, int* partials, Launch launch) {
   return b.n || !*partials ? flush() : LORA_OK;
 }
 
+// What the sum leaves in L2 for the scaling.  97 MB that were not there before take 47.3 us with 0 (as without any
+// policy), 47.0 with 40 MB, 44.9 with 60, 44.4 with 80; the same 97 MB call after call 43.0, 40.8, 39.8 and 41.1.
+constexpr double kClipKeepBytes = 60e6;
+
 int clip_check(const lora_grad* grads, int n, size_t* bytes) {
   if (!grads) return LORA_ENULL;
   if (n < 1 || n > 65536) return LORA_EINVAL;
@@ -2843,9 +2847,12 @@ int lora_clip_grads(const lora_grad* grads, int n_grads, float max_norm, float* 
   int partials = 0, again = 0;
   const bool one_batch = n_grads <= kClipTensors;
   bool done = false;
+  double total = 1.0;
+  for (int i = 0; i < n_grads; ++i) total += (double)grads[i].n * (grads[i].dtype == LORA_BF16 ? 2 : 4);
+  const float keep = (float)std::min(1.0, kClipKeepBytes / total);
   rc = clip_batches(grads, n_grads, &partials, [&](const ClipBatch& b, int first, int ctas) {
     done = one_batch && clip_is_small(b);
-    return (done ? launch_clip_one(b, max_norm, norm, coef, st) : launch_clip_sum(b, partial + first, ctas, st)) ==
+    return (done ? launch_clip_one(b, max_norm, norm, coef, st) : launch_clip_sum(b, partial + first, ctas, keep, st)) ==
                    cudaSuccess
                ? LORA_OK
                : LORA_ECUDA;

@@ -9,10 +9,13 @@
 //   clip_sum_kernel    the CTAs' sums of squares, one CTA per SM
 //   clip_scale_kernel  every CTA adds these up again in the same order, then scales, from the last piece to the first:
 //                      what was read last is still in L2
-// All are bound by memory (a read for the norm, a read from L2 or HBM and a write for the scaling).  FP64 is scarce
-// on this GPU (about 2 operations a clock and SM), so a lane's 16 squares are summed in fp32 and these sums as pairs
-// of fp32; only the warps' sums are added in fp64.  The tensors' table is a kernel argument: no copy precedes the
-// launches.
+// Many tensors are bound by memory: a read for the norm, a read from L2 or HBM and a write for the scaling.  What the
+// sum reads last is asked to stay in L2, all else to leave first (28 layers of 16 tensors, 97 MB: 39.8 us call after
+// call, 44.9 where nothing was in L2 before; 194 MB at the copy rate take 28.7, 291 take 43).  Few tensors are bound by
+// the chain launch, load, sum, exchange, store: 4.5 us for four tensors, 0.66 MB.
+// FP64 is scarce on this GPU (about 2 operations a clock and SM), so a lane's 16 squares are summed in fp32 and these
+// sums as pairs of fp32; only the warps' sums are added in fp64.  The tensors' table is a kernel argument: no copy
+// precedes the launches.
 #include <type_traits>
 
 #include "common.cuh"
@@ -24,7 +27,7 @@ namespace {
 
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
 constexpr int kScaleWarps = 16;  // of the scaling, one CTA per SM: their registers hold what is on its way
-constexpr int kOneCtas = 16;  // of the single cluster
+constexpr int kOneCtas = 16;     // of the single cluster
 
 // A piece's place: the elements before the first 16-byte boundary of src (head), the vectors behind them, the rest.
 struct Piece {
@@ -76,12 +79,32 @@ __device__ __forceinline__ int edge_index(const Piece& p, int lane) {
   return i < p.n ? i : -1;
 }
 
+// L2 policies: what stays for the scaling, and what is read for the last time or will not stay anyway.
+__device__ __forceinline__ uint64_t policy_keep() {
+  uint64_t v;
+  asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(v));
+  return v;
+}
+__device__ __forceinline__ uint64_t policy_pass() {
+  uint64_t v;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(v));
+  return v;
+}
+__device__ __forceinline__ uint4 load_vec(const uint4* p, uint64_t policy) {
+  uint4 v;
+  asm volatile("ld.global.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p), "l"(policy)
+               : "memory");
+  return v;
+}
+
 template <int PART>
-__device__ __forceinline__ void load_piece(const Piece& p, int lane, Held& h) {
+__device__ __forceinline__ void load_piece(const Piece& p, int lane, Held& h, uint64_t policy) {
   const uint4* v = reinterpret_cast<const uint4*>(p.src + (p.head << (p.half ? 1 : 2))) + lane + 32 * kVecs * PART;
   const int left = p.vecs - lane - 32 * kVecs * PART;
 #pragma unroll
-  for (int q = 0; q < kVecs; ++q) h.v[q] = 32 * q < left ? v[32 * q] : make_uint4(0u, 0u, 0u, 0u);
+  for (int q = 0; q < kVecs; ++q) h.v[q] = 32 * q < left ? load_vec(v + 32 * q, policy) : make_uint4(0u, 0u, 0u, 0u);
   h.edge = 0u;
   if (PART == 0) {
     const int e = edge_index(p, lane);
@@ -132,7 +155,7 @@ struct Squares {
     uint32_t any = h.edge;
 #pragma unroll
     for (int q = 0; q < kVecs; ++q) any |= h.v[q].x | h.v[q].y | h.v[q].z | h.v[q].w;
-    lost = lost || s != 0.f || (any & 0x7fff7fffu) != 0u;
+    lost = lost || s != 0.f || (any & (p.half ? 0x7fff7fffu : 0x7fffffffu)) != 0u;  // but for signs
   }
 };
 
@@ -151,13 +174,14 @@ __device__ __forceinline__ double scaled_squares(const Held& h, bool half) {
 template <typename Table>
 __device__ __noinline__ double slow_squares(const Table& b, int c, int c1) {
   const int lane = threadIdx.x & 31;
+  const uint64_t pass = policy_pass();
   double sum = 0.0;
   for (; c < c1; c += kWarps) {
     const Piece p = piece_of(b.t[find_tensor(b, c)], c);
     Held h;
-    load_piece<0>(p, lane, h);
+    load_piece<0>(p, lane, h, pass);
     sum += scaled_squares(h, p.half);
-    load_piece<1>(p, lane, h);
+    load_piece<1>(p, lane, h, pass);
     sum += scaled_squares(h, p.half);
   }
   return sum;
@@ -283,29 +307,33 @@ __device__ __forceinline__ void run_of(int chunks, int* c0, int* c1) {
 
 template <typename Table>
 __global__ void __launch_bounds__(kThreads) clip_sum_kernel(const __grid_constant__ Table b,
-                                                            double* __restrict__ partial) {
+                                                            double* __restrict__ partial, float keep) {
   griddep_wait();
   griddep_launch_dependents();
   __shared__ double part[kWarps];
   const int lane = threadIdx.x & 31;
   int c0, c1;
   run_of(b.chunks, &c0, &c1);
+  // the run's end stays in L2, where the scaling begins
+  const uint64_t pass = policy_pass(), hold = policy_keep();
+  const int from = c1 - (int)(keep * (float)(c1 - c0));
+  auto policy = [&](int c) { return c >= from ? hold : pass; };
   Squares squares;
   int c = c0 + (int)(threadIdx.x >> 5);
   if (c < c1) {
     int i = find_tensor(b, c);
     Piece p = piece_of(b.t[i], c);
     Held h0, h1;
-    load_piece<0>(p, lane, h0);
+    load_piece<0>(p, lane, h0, policy(c));
     while (c < c1) {
       const Piece now = p;
-      load_piece<1>(now, lane, h1);
+      load_piece<1>(now, lane, h1, policy(c));
       squares.add(now, h0);
       c += kWarps;
       if (c < c1) {
         while (i + 1 < b.n && c >= b.t[i + 1].chunk_begin) ++i;
         p = piece_of(b.t[i], c);
-        load_piece<0>(p, lane, h0);
+        load_piece<0>(p, lane, h0, policy(c));
       }
       squares.add(now, h1);
     }
@@ -315,12 +343,12 @@ __global__ void __launch_bounds__(kThreads) clip_sum_kernel(const __grid_constan
 }
 
 template <typename Table>
-__global__ void __launch_bounds__(32 * kScaleWarps) clip_scale_kernel(const __grid_constant__ Table b,
-                                                              const double* __restrict__ partial, int n_partial,
-                                                              float max_norm, float* __restrict__ norm_out,
-                                                              float* __restrict__ coef_out) {
+__global__ void __launch_bounds__(32 * kScaleWarps)
+    clip_scale_kernel(const __grid_constant__ Table b, const double* __restrict__ partial, int n_partial, float max_norm,
+                      float* __restrict__ norm_out, float* __restrict__ coef_out) {
   __shared__ Coef s_coef;
   const int lane = threadIdx.x & 31;
+  const uint64_t pass = policy_pass();
   int c0, c1;
   run_of(b.chunks, &c0, &c1);
   // the tensors were written before the first launch of the call began
@@ -330,7 +358,7 @@ __global__ void __launch_bounds__(32 * kScaleWarps) clip_scale_kernel(const __gr
   if (c >= c0) {
     i = find_tensor(b, c);
     p = piece_of(b.t[i], c);
-    load_piece<0>(p, lane, h0);
+    load_piece<0>(p, lane, h0, pass);
   }
   griddep_wait();
   griddep_launch_dependents();
@@ -344,13 +372,13 @@ __global__ void __launch_bounds__(32 * kScaleWarps) clip_scale_kernel(const __gr
   const Coef cf = s_coef;
   while (c >= c0) {
     const Piece now = p;
-    load_piece<1>(now, lane, h1);
+    load_piece<1>(now, lane, h1, pass);
     store_piece<0>(now, lane, h0, cf);
     c -= kScaleWarps;
     if (c >= c0) {
       while (c < b.t[i].chunk_begin) --i;
       p = piece_of(b.t[i], c);
-      load_piece<0>(p, lane, h0);
+      load_piece<0>(p, lane, h0, pass);
     }
     store_piece<1>(now, lane, h1, cf);
   }
@@ -372,8 +400,8 @@ __global__ void __launch_bounds__(kThreads) clip_one_kernel(const __grid_constan
   Squares squares;
   if (c < b.chunks) {
     p = piece_of(b.t[find_tensor(b, c)], c);
-    load_piece<0>(p, lane, h0);
-    load_piece<1>(p, lane, h1);
+    load_piece<0>(p, lane, h0, policy_pass());
+    load_piece<1>(p, lane, h1, policy_pass());
     squares.add(p, h0);
     squares.add(p, h1);
   }
@@ -442,6 +470,8 @@ cudaError_t with_table(const ClipBatch& b, Fn fn) {
 
 }  // namespace
 
+// One launch or two (us): 16384 elements 3.6 and 4.9, 131072 4.2 and 5.1, 262144 5.3 and 5.1 (with a launch less for
+// the host), 524288 7.9 and 5.3.
 bool clip_is_small(const ClipBatch& b) { return b.chunks <= kOneCtas * kWarps / 2; }
 
 // A quarter of a CTA's warps at work are enough to keep its loads in flight; more CTAs cost more partial sums.
@@ -450,9 +480,9 @@ int clip_ctas(int chunks, int num_sms) {
   return n < 1 ? 1 : n < num_sms ? n : num_sms;
 }
 
-cudaError_t launch_clip_sum(const ClipBatch& b, double* partial, int ctas, cudaStream_t st) {
+cudaError_t launch_clip_sum(const ClipBatch& b, double* partial, int ctas, float keep, cudaStream_t st) {
   return with_table(b, [&](const auto& t) {
-    return launch_kernel(clip_sum_kernel<std::decay_t<decltype(t)>>, dim3(ctas), dim3(kThreads), 0, st, 1, t, partial);
+    return launch_kernel(clip_sum_kernel<std::decay_t<decltype(t)>>, dim3(ctas), dim3(kThreads), 0, st, 1, t, partial, keep);
   });
 }
 
@@ -470,8 +500,7 @@ cudaError_t launch_clip_one(const ClipBatch& b, float max_norm, float* norm, flo
     static std::atomic<unsigned long long> done{0};
     const cudaError_t e = allow_cluster_once(clip_one_kernel<T>, done);
     if (e != cudaSuccess) return e;
-    return launch_kernel(clip_one_kernel<std::decay_t<decltype(t)>>, dim3(kOneCtas), dim3(kThreads), 0, st, kOneCtas,
-                         t, max_norm, norm, coef);
+    return launch_kernel(clip_one_kernel<T>, dim3(kOneCtas), dim3(kThreads), 0, st, kOneCtas, t, max_norm, norm, coef);
   });
 }
 

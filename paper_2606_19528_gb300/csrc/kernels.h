@@ -509,7 +509,8 @@ struct ClipBatch {
 };
 // partial[0 .. ctas) = the CTAs' sums of squares over the batch; ctas = clip_ctas(chunks, num_sms).
 int clip_ctas(int chunks, int num_sms);
-cudaError_t launch_clip_sum(const ClipBatch& b, double* partial, int ctas, cudaStream_t stream);
+// keep: the share of each CTA's elements, from the end, that is to stay in L2 for the scaling.
+cudaError_t launch_clip_sum(const ClipBatch& b, double* partial, int ctas, float keep, cudaStream_t stream);
 // dst = src min(1, max_norm / norm) over the batch, norm from partial[0 .. n_partial).
 cudaError_t launch_clip_scale(const ClipBatch& b, const double* partial, int n_partial, float max_norm, float* norm,
                               float* coef, int ctas, cudaStream_t stream);

@@ -125,6 +125,17 @@ def test_whole_range_of_fp32(std):
     check(mixed, [torch.empty_like(g) for g in mixed], 1e-3)
 
 
+@pytest.mark.parametrize("bits", [1, 0x8000, 0x7FFFFF])
+def test_subnormals_alone(bits):
+    """Elements of one bit pattern each; the norm is a subnormal or a little above: one spacing, and the root's rounding."""
+    n = 4999
+    g = torch.full((n,), bits, dtype=torch.int32, device="cuda").view(torch.float32)
+    out = torch.empty_like(g)
+    norm, coef = run([(g, out)], 1.0)
+    assert abs(norm - bits * 2.0**-149 * math.sqrt(n)) <= 2.0**-149 + 1e-6 * norm
+    assert coef == 1.0 and torch.equal(out.view(torch.int32), g.view(torch.int32))
+
+
 def test_large_values_in_one_place():
     """One element whose square overflows among small ones of the same thread's."""
     g = torch.full((30000,), 1e-3, device="cuda")
