@@ -240,14 +240,17 @@ __global__ void __launch_bounds__(kMostThreads) decode_kernel(const __grid_const
       mma_bf16(acc[0][m], adapter[0], adapter[1], adapter[2], adapter[3], lo.z, hi.z);
     }
   }
-  __shared__ float red[kMostThreads / 32][NT * 8][kRedPitch];
+  // the warps' sums: [warp][token][row], as large as the block's warps need
+  extern __shared__ float red_words[];
+  auto red = reinterpret_cast<float(*)[NT * 8][kRedPitch]>(red_words);
 #pragma unroll
   for (int m = 0; m < NT; ++m)
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       red[warp][8 * m + 2 * t + (e & 1)][g + 8 * (e >> 1)] = kChains == 2 ? acc[0][m][e] + acc[kChains - 1][m][e] : acc[0][m][e];
-  __shared__ float su_red[OWN ? kMostThreads / 32 : 1][NT * 8][kRedPitch], s_su[NT * 8][16], s_b[kTileN][17];
+  __shared__ float s_su[OWN ? NT * 8 : 1][16], s_b[OWN ? kTileN : 1][17];
   if constexpr (OWN) {
+    const auto su_red = red + warps;
 #pragma unroll
     for (int m = 0; m < NT; ++m)
 #pragma unroll
@@ -279,20 +282,23 @@ __global__ void __launch_bounds__(kMostThreads) decode_kernel(const __grid_const
 }
 
 cudaError_t launch_narrow(DecodeBatch& b, int most, bool own, int num_sms, cudaStream_t st) {
-  int tiles = 0, chunks = 1;
+  int tiles = 0, chunks = 1, adapter = 0;  // steps of a block's warps: chunks, and 16 adapter columns
   for (int i = 0; i < b.n; ++i) {
     b.p[i].tile_begin = tiles;
     tiles += (b.p[i].N + kTileN - 1) / kTileN;
     chunks = std::max(chunks, (b.p[i].K + kChunk - 1) / kChunk);
+    if (!own) adapter = std::max(adapter, su_steps(b.p[i].r));
   }
-  // The steps of a warp, and about a quarter of one for each warp that a block's sums come from, times the waves of
-  // blocks (about 30 warps fit an SM).  (3072 x 5120: 8 warps 5.4, 4: 6.7 us; 8192 x 3072: 16: 7.5, 8: 8.5, 4: 12.6 us;
-  // 2048 x 11008: 4: 6.1, 8: 7.6, 2: 8.0 us)
+  // The steps of a warp (of the adapter's, half), and a quarter of one for each warp that a block's sums come from, times
+  // the waves of blocks, of which an SM's registers hold so many (32 warps with 8 tokens, 28 with 16).  (3072 x 5120: 8
+  // warps 5.4, 4: 6.7 us; 8192 x 3072: 16: 7.5, 8: 8.5, 4: 12.6; 2048 x 11008: 4: 6.1, 8: 7.6, 2: 8.0; nine tokens,
+  // 8192 x 3072: 16, in two waves, 14.8, 13: 11.7; 16 tokens, 64 x 9565, r 128: 1: 11.9, 4: 6.8)
+  const int fit = most <= 8 ? 32 : 28;
   int warps = 1;
   double least = 0.0;
-  for (int w = 1; w <= kMostThreads / 32 && w <= chunks; ++w) {
-    const long long waves = ((long long)tiles * w + 30 * num_sms - 1) / (30 * num_sms);
-    const double cost = (double)waves * ((chunks + w - 1) / w + 0.25 * w);
+  for (int w = 1; w <= kMostThreads / 32 && w <= std::max(chunks, adapter); ++w) {
+    const long long at_once = (long long)(fit / w) * num_sms, waves = (tiles + at_once - 1) / at_once;
+    const double cost = (double)waves * ((chunks + w - 1) / w + 0.5 * ((adapter + w - 1) / w) + 0.25 * w);
     if (w == 1 || cost < least) {
       warps = w;
       least = cost;
@@ -303,7 +309,8 @@ cudaError_t launch_narrow(DecodeBatch& b, int most, bool own, int num_sms, cudaS
     const auto kernel = own         ? decode_kernel<1, true, Table>
                         : most <= 8 ? decode_kernel<1, false, Table>
                                     : decode_kernel<2, false, Table>;
-    return launch_kernel(kernel, dim3(tiles), dim3(32 * warps), 0, st, 1, t);
+    const size_t smem = (size_t)(own ? 2 : 1) * warps * (most <= 8 ? 8 : 16) * kRedPitch * sizeof(float);
+    return launch_kernel(kernel, dim3(tiles), dim3(32 * warps), smem, st, 1, t);
   });
 }
 
@@ -319,24 +326,25 @@ cudaError_t launch_su(const DecodeBatch& b, int most, cudaStream_t st) {
   });
 }
 
-// Which second launch a group of projections takes, by their times as measured (us): 16-row blocks read their bytes at
-// 4.3 TB/s for one token, 3 for eight and 1.8 for sixteen, and are there at once; the wide launch takes 0.475 for a
-// panel of 128 rows whatever the tokens, and starts late.  (3072 x 128256, 1 and 16 tokens: blocks 52 and 117, wide 44
-// and 45; 3072 x 16384: 9.0 and 19, 10.9 and 11.3; 8192 x 3072: 8.4 and 13.7, 19 and 20; 4096 x 16384, 8 tokens: 15.5,
-// 13.0.)
+// Which second launch a group of projections takes, by their times as measured (us).  16-row blocks, dealt evenly to the
+// SMs, read their bytes at 4.3 TB/s for one token, 3 for eight and 1.8 for sixteen, and are there at once; plan_wide() has
+// the wide launch's.  (Blocks and wide, 3072 x 128256, 1 token: 52 and 44, 16: 117 and 45; 4096 x 16384, r 16, 1 token:
+// 12.7 and 14.6, 8: 15.9 and 14.7, 16: 22 and 15; 8192 x 8192, r 16, 1 token: 13.0 and 15.0, 8: 16.3 and 15.2, 16: 26 and
+// 15.7; two of 2048 x 11008, r 64, 8 tokens: 13.3 and 16.1, 9: 20 and 16.1; 8192 x 3072, r 16, 8 tokens: 9.7 and 10.6, 16:
+// 14.0 and 11.7; 3072 x 3072, r 16, 16 tokens: 7.1 and 8.3.)
 bool wide_pays(const DecodeBatch& b, int num_sms) {
   const int T = b.p[0].T, K = b.p[0].K;
-  double mb = 0.0;
-  long long tiles = 0;
-  int adapters = 0;
+  long long tiles = 0, blocks = 0;
+  int rank = 0;
   for (int i = 0; i < b.n; ++i) {
-    mb += (double)b.p[i].N * K * (0.5625e-6);
     tiles += (b.p[i].N + 127) / 128;
-    adapters |= b.p[i].r > 0;
+    blocks += (b.p[i].N + kTileN - 1) / kTileN;
+    rank = std::max(rank, b.p[i].r);
   }
-  const double blocks = 2.6 + mb * (T <= 8 ? 0.22 + 0.0155 * T : 0.27 + 0.018 * T);
-  const double wide = 4.6 + (double)((tiles + num_sms - 1) / num_sms) * ((K + 255) / 256 + adapters) * 0.475;
-  return wide < blocks;
+  const double each = (double)((blocks + num_sms - 1) / num_sms);  // of an SM
+  const double mb = each * num_sms * kTileN * K * 0.5625e-6;
+  const double us = 2.6 + 0.085 * each + mb * (T <= 8 ? 0.22 + 0.0155 * T : 0.27 + 0.018 * T) + 0.02 * rank;
+  return plan_wide(tiles, (K + 255) / 256, rank, num_sms).us < us;
 }
 
 // Whether the blocks compute su themselves, with all of A read by each of them, against a launch before theirs: a

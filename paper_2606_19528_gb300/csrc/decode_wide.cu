@@ -12,8 +12,10 @@
 //   warps 8-19   three groups that dequantize every third panel each, into a buffer of their own
 // The adapter is one more step of a tile: the group's threads store their rows of B, and the stage holds su's three
 // terms as the MMAs' B operand.
-// Handing a panel over in two or four parts makes the call slower (50 and 70 us where this takes 43: each part costs
-// the MMAs some 200 clocks between them).
+// A call whose tiles are fewer than the SMs has clusters of CTAs share a tile's columns; their sums meet in the first
+// one's shared memory (plan_wide).
+// 16 tokens, 128256 x 3072, 222 MB: 45 us, 4.9 TB/s, bound by the dequantization's instructions and the hand-over of the
+// panels (each costs the MMAs some 200 clocks; handing a panel over in two or four parts takes 50 and 70 us).
 #include <algorithm>
 
 #include "common.cuh"
@@ -31,6 +33,8 @@ constexpr uint32_t kDCol = kGroups * kBufCols, kTmemCols = 512;  // behind them 
 constexpr int kMaxStages = 9;
 constexpr long long kDrainNs = 100000000ll;
 constexpr int kMostSmem = 227 * 1024;
+constexpr uint32_t kSumBytes = kTok * kRows * 4;  // of a CTA's sums of a tile
+constexpr int kMostSplit = 8;
 
 struct Ctl {
   uint64_t full[kMaxStages], empty[kMaxStages];
@@ -67,7 +71,8 @@ struct CodeMaps {
 
 struct Wide {
   int tiles, stages;
-  int held;  // 1: the whole activation stays in shared memory, behind the stages; 0: a stage carries its columns
+  int held;   // bytes of the activation (a CTA's columns) that stay in shared memory; 0: a stage carries its columns
+  int split;  // CTAs of a cluster that share a tile's columns (then one tile per cluster)
 };
 
 template <typename Table>
@@ -77,10 +82,16 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
                                                                   const __grid_constant__ Wide wide) {
   extern __shared__ __align__(1024) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int T = b.p[0].T, K = b.p[0].K, panels = (K + kPanel - 1) / kPanel, pairs = K / 64;
+  const int T = b.p[0].T, K = b.p[0].K, pairs = K / 64;
+  // the CTA's tiles, and its panels of them, the c0-th on; the adapter is the first CTA's, whose share is the smallest
+  const int split = wide.split, rank = (int)blockIdx.x % split;
+  const int tile0 = (int)blockIdx.x / split, stride = (int)gridDim.x / split;
+  const int all = (K + kPanel - 1) / kPanel, c0 = all * rank / split, panels = all * (rank + 1) / split - c0;
   const uint32_t stage_bytes = kCodeBytes + (wide.held ? 0u : kXBytes);
   const uint32_t ring = smem_u32(smem), held = ring + wide.stages * stage_bytes;
-  Ctl* ctl = reinterpret_cast<Ctl*>(smem + wide.stages * stage_bytes + (wide.held ? panels * kXBytes : 0u));
+  uint8_t* rest = smem + wide.stages * stage_bytes + wide.held;
+  float* sums = reinterpret_cast<float*>(rest);  // [split][tokens][rows], the first CTA's: the others' sums come here
+  Ctl* ctl = reinterpret_cast<Ctl*>(rest + (split > 1 ? split * kSumBytes : 0u));
   volatile int* abort = &ctl->abort;
   const WaitCtl wait{b.status, b.limit_ns};
   const uint32_t full = smem_u32(ctl->full), empty = smem_u32(ctl->empty), afull = smem_u32(ctl->afull);
@@ -112,6 +123,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  if (split > 1) cluster_sync_all();  // every CTA has begun: its shared memory may be written
   griddep_launch_dependents();
   const uint32_t tmem = ctl->tmem;
   long long issued = 0;     // producer: stages
@@ -132,7 +144,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
         phase ^= 1u;
       }
     };
-    for (int tile = blockIdx.x; tile < wide.tiles && ok; tile += gridDim.x, first = false) {
+    for (int tile = tile0; tile < wide.tiles && ok; tile += stride, first = false) {
       while (proj + 1 < b.n && tile >= b.p[proj + 1].tile_begin) ++proj;
       const DecodeProj& p = b.p[proj];
       const int n0 = (tile - p.tile_begin) * kRows;
@@ -141,14 +153,14 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
           const uint32_t at = ring + s * stage_bytes, bar = full + 8 * s;
           const bool with_x = !wide.held || first;  // the held activation comes with the first tile's codes
           mbar_arrive_expect_tx(bar, kCodeBytes + (with_x ? kXBytes : 0u));
-          tma_load_2d(at, &maps.codes[proj], bar, c * (kPanel / 2), n0);
+          tma_load_2d(at, &maps.codes[proj], bar, (c0 + c) * (kPanel / 2), n0);
           if (with_x)
             for (int i = 0; i < kPanel / 64; ++i)
               tma_load_2d((wide.held ? held + c * kXBytes : at + kCodeBytes) + i * kXBlock, &x_map, bar,
-                          c * kPanel + 64 * i, 0);
+                          (c0 + c) * kPanel + 64 * i, 0);
         }
       }
-      if (p.r > 0 && claim()) {
+      if (p.r > 0 && rank == 0 && claim()) {
         if (!waited) {
           griddep_wait();  // su
           waited = true;
@@ -194,9 +206,9 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
         aphase ^= 1u;
       }
     };
-    for (int tile = blockIdx.x; tile < wide.tiles && ok; tile += gridDim.x, ++n) {
+    for (int tile = tile0; tile < wide.tiles && ok; tile += stride, ++n) {
       while (proj + 1 < b.n && tile >= b.p[proj + 1].tile_begin) ++proj;
-      const int d = n & 1, r = b.p[proj].r;
+      const int d = n & 1, r = rank == 0 ? b.p[proj].r : 0;
       if (!wait_all(dempty + 8 * d, (uint32_t)((n >> 1) & 1) ^ 1u)) break;
       tc_fence_after();
       const uint32_t d_tmem = tmem + kDCol + (uint32_t)(d * kTok);
@@ -228,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
   } else if (warp >= 4 && warp < 8) {  // ------------------------------------- epilogue
     const int q = warp & 3;
     int proj = 0, n = 0;
-    for (int tile = blockIdx.x; tile < wide.tiles; tile += gridDim.x, ++n) {
+    for (int tile = tile0; tile < wide.tiles; tile += stride, ++n) {
       while (proj + 1 < b.n && tile >= b.p[proj + 1].tile_begin) ++proj;
       const DecodeProj& p = b.p[proj];
       const int d = n & 1, row = (tile - p.tile_begin) * kRows + q * 32 + lane;
@@ -241,7 +253,12 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(dempty + 8 * d);
-      if (row < p.N) {
+      if (split > 1) {
+        const uint32_t to = mapa_shared(smem_u32(sums), 0) + (uint32_t)rank * kSumBytes + (uint32_t)(q * 32 + lane) * 4u;
+#pragma unroll
+        for (int e = 0; e < kTok; ++e)
+          if (e < T) st_cluster_u32(to + (uint32_t)(e * kRows) * 4u, v[e]);
+      } else if (row < p.N) {
 #pragma unroll
         for (int e = 0; e < kTok; ++e)
           if (e < T) p.y[(long long)e * p.N + row] = __float2bfloat16(__uint_as_float(v[e]) * 0x1p40f);
@@ -250,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
   } else if (warp >= 8) {  // ------------------------------------------------- dequantization
     const int group = (warp - 8) / 4, q = warp & 3, row = q * 32 + lane;
     // the group's next step: panel c of a tile (c == panels: the adapter), and its (s, b) pairs, loaded a step ahead
-    int tile = blockIdx.x, c = group, proj = 0, steps = 0;
+    int tile = tile0, c = group, proj = 0, steps = 0;
     const uint32_t* pair_at = nullptr;
     const __nv_bfloat16* adapter = nullptr;  // the row's
     bool in_row = false;
@@ -259,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
       while (proj + 1 < b.n && tile >= b.p[proj + 1].tile_begin) ++proj;
       const DecodeProj& p = b.p[proj];
       const int n = (tile - p.tile_begin) * kRows + row;
-      steps = panels + (p.r > 0);
+      steps = panels + (p.r > 0 && rank == 0);
       in_row = n < p.N;
       pair_at = reinterpret_cast<const uint32_t*>(p.params) + (long long)n * pairs;
       adapter = p.B + (long long)n * p.r;
@@ -267,7 +284,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
     auto settle = [&]() {
       while (tile < wide.tiles && c >= steps) {
         c -= steps;
-        tile += gridDim.x;
+        tile += stride;
         open();
       }
     };
@@ -275,7 +292,10 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
     auto fetch = [&]() {
       if (tile >= wide.tiles || c == panels) return;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) next[i] = in_row && 4 * c + i < pairs ? __ldg(pair_at + 4 * c + i) : 0u;
+      for (int i = 0; i < 4; ++i) {
+        const int at = 4 * (c0 + c) + i;
+        next[i] = in_row && at < pairs ? __ldg(pair_at + at) : 0u;
+      }
     };
     open();
     settle();
@@ -376,6 +396,24 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
     }
   }
 
+  if (split > 1) {  // ------------------------------------------------------- the cluster's sums, in the order of its CTAs
+    __syncwarp();
+    cluster_sync_all();
+    if (rank == 0) {
+      int proj = 0;
+      while (proj + 1 < b.n && tile0 >= b.p[proj + 1].tile_begin) ++proj;
+      const DecodeProj& p = b.p[proj];
+      const int n0 = (tile0 - p.tile_begin) * kRows, rows = min(kRows, p.N - n0);
+      for (int o = threadIdx.x; o < kRows * T; o += kThreads) {
+        const int e = o / kRows, i = o % kRows;
+        if (i >= rows) continue;
+        float v = 0.f;
+        for (int k = 0; k < split; ++k) v += sums[(k * kTok + e) * kRows + i];
+        p.y[(long long)e * p.N + n0 + i] = __float2bfloat16(v * 0x1p40f);
+      }
+    }
+  }
+
   // ------------------------------------------------------------------------- teardown
   tc_fence_before();
   __syncthreads();
@@ -399,23 +437,73 @@ __global__ void __launch_bounds__(kThreads, 1) decode_wide_kernel(const __grid_c
 
 }  // namespace
 
+namespace {
+
+// Clusters of `ctas` CTAs that run at once: one CTA per SM, a cluster within one of the GPU's groups of SMs.
+int most_clusters(int ctas) {
+  static std::atomic<int> cache[64][kMostSplit + 1];  // 0: not asked yet
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  std::atomic<int>& known = cache[dev & 63][ctas];
+  int n = known.load(std::memory_order_relaxed);
+  if (n) return n;
+  static std::atomic<unsigned long long> done{0};
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kMostSmem;
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)ctas;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (set_smem_once(decode_wide_kernel<DecodeTable<8>>, kMostSmem, done) != cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&n, decode_wide_kernel<DecodeTable<8>>, &cfg) != cudaSuccess)
+    return 0;
+  known.store(std::max(n, 1), std::memory_order_relaxed);
+  return n;
+}
+
+}  // namespace
+
+// The launch starts late (tensor memory, the first panels), each step of a CTA, a panel or the adapter, takes 0.475 us
+// whatever the tokens, and the adapter waits for the launch before.  Where tiles leave SMs idle, the CTAs of a cluster
+// share a tile's panels.  (Alone and shared: 8192 x 8192, r 16, 16 tokens, 20.8 and 15.7 us by two; 8192 x 3072 20.3 and
+// 11.7 by five; 5120 rows of 3072 11.0 and 9.7 by three; six for 3072 rows, one cluster more than run at once, 18.8.)
+WidePlan plan_wide(long long tiles, int panels, int rank, int num_sms) {
+  const int adapter = rank > 0;
+  const double late = adapter * 1.6 + 0.02 * rank;
+  WidePlan best{1, 4.6 + late + (double)((tiles + num_sms - 1) / num_sms) * (panels + adapter) * 0.475};
+  for (int s = 2; s <= kMostSplit && s <= panels; ++s) {
+    const double us = 4.9 + late + 0.8 * adapter + std::max((panels + s - 1) / s, panels / s + adapter) * 0.475;
+    if (us < best.us && tiles <= num_sms / s && tiles <= most_clusters(s)) best = WidePlan{s, us};
+  }
+  return best;
+}
+
 cudaError_t launch_decode_wide(DecodeBatch& b, int num_sms, cudaStream_t st) {
   const DecodeProj& p0 = b.p[0];
   const int panels = (p0.K + kPanel - 1) / kPanel;
   Wide w;
   w.tiles = 0;
+  int rank = 0;
   for (int i = 0; i < b.n; ++i) {
+    rank = std::max(rank, b.p[i].r);
     b.p[i].tile_begin = w.tiles;
     w.tiles += (b.p[i].N + kRows - 1) / kRows;
   }
   CUtensorMap x_map;
   if (!make_bf16_map(&x_map, p0.x, p0.K, p0.T, 64, kTok)) return cudaErrorInvalidValue;
+  w.split = plan_wide(w.tiles, panels, rank, num_sms).split;
   // the activation is held where at least two stages of codes per group fit beside it
-  const int room = kMostSmem - (int)sizeof(Ctl), all = panels * (int)kXBytes;
-  w.held = all + 2 * kGroups * (int)kCodeBytes <= room;
+  const int sums = w.split > 1 ? w.split * (int)kSumBytes : 0, room = kMostSmem - (int)sizeof(Ctl) - sums;
+  const int all = (panels + w.split - 1) / w.split * (int)kXBytes;
+  w.held = all + 2 * kGroups * (int)kCodeBytes <= room ? all : 0;
   const int stage = kCodeBytes + (w.held ? 0 : kXBytes);
-  w.stages = std::min(kMaxStages, (room - (w.held ? all : 0)) / stage) / kGroups * kGroups;
-  const size_t smem = (size_t)w.stages * stage + (w.held ? all : 0) + sizeof(Ctl);
+  w.stages = std::min(kMaxStages, (room - w.held) / stage) / kGroups * kGroups;
+  const size_t smem = (size_t)w.stages * stage + w.held + sums + sizeof(Ctl);
+  const int ctas = w.split > 1 ? w.tiles * w.split : std::min(w.tiles, num_sms);
   return with_table(b, [&](const auto& t) {
     using Table = std::decay_t<decltype(t)>;
     CodeMaps<Table::kCap> maps;
@@ -425,8 +513,7 @@ cudaError_t launch_decode_wide(DecodeBatch& b, int num_sms, cudaStream_t st) {
     static std::atomic<unsigned long long> done{0};
     const cudaError_t e = set_smem_once(decode_wide_kernel<Table>, kMostSmem, done);
     if (e != cudaSuccess) return e;
-    return launch_kernel(decode_wide_kernel<Table>, dim3(std::min(w.tiles, num_sms)), dim3(kThreads), smem, st, 1, t, maps,
-                         x_map, w);
+    return launch_kernel(decode_wide_kernel<Table>, dim3(ctas), dim3(kThreads), smem, st, w.split, t, maps, x_map, w);
   });
 }
 

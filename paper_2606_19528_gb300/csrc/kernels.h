@@ -458,6 +458,12 @@ bool make_bf16_map(CUtensorMap* m, const void* ptr, int width, int rows, int box
 cudaError_t launch_decode(DecodeBatch& b, int num_sms, cudaStream_t stream);
 // Its second launch for many rows (decode_wide.cu), of projections with one activation.
 cudaError_t launch_decode_wide(DecodeBatch& b, int num_sms, cudaStream_t stream);
+// The CTAs that share each of its tiles of 128 rows (panels of 256 columns; the largest rank), and its time.
+struct WidePlan {
+  int split;
+  double us;
+};
+WidePlan plan_wide(long long tiles, int panels, int rank, int num_sms);
 
 // ---------------------------------------------------------------- policy and preference losses
 struct ObjectiveSeq {  // what the first launch leaves per sequence (policy) or pair (preference), sums as fp32 pairs

@@ -179,7 +179,7 @@ def test_same_bits_every_time_and_on_another_stream():
 
 @pytest.mark.parametrize("T,K,N", [(16, 3072, 30000), (16, 1024, 20001), (8, 3072, 30000), (9, 320, 50000),
                                    (16, 6144, 6000), (3, 11008, 2048), (16, 12288, 1000), (16, 4416, 40001),
-                                   (13, 64, 200003)])
+                                   (13, 64, 200003), (16, 8192, 3000), (9, 16448, 1000), (16, 8192, 9000)])
 def test_many_tiles_come_out_the_same_in_every_call(T, K, N):
     """Every SM takes many tiles through its rings, with little room for them beside 16 tokens: 100 calls, bit for
     bit, and against the product in fp32."""
@@ -239,7 +239,10 @@ def test_chain_of_calls_in_a_graph():
 
 @pytest.mark.parametrize("T,K,shapes", [
     (16, 1024, [(40001, 16), (30000, 0), (129, 128), (2500, 13)]), (1, 4160, [(90001, 64)]), (9, 192, [(150000, 1), (7, 3)]),
-    (12, 8192, [(20011, 128), (20000, 0)])])
+    (12, 8192, [(20011, 128), (20000, 0)]),
+    # tiles whose columns are shared out
+    (16, 8192, [(3000, 16)]), (16, 8192, [(8191, 7)]), (11, 8256, [(5000, 24), (1000, 0)]), (16, 16448, [(1000, 13)]),
+    (13, 16384, [(130, 128)]), (16, 12288, [(2200, 0)])])
 def test_many_rows_with_adapters(T, K, shapes):
     """Projections of tens of thousands of rows that share an activation, with adapters of any rank or none: the
     launch for many rows, against fp32 products (the bound of the module's head, twice the sums' part)."""
