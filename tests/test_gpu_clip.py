@@ -2,7 +2,7 @@
 fp64 oracle.
 
 Tolerances: squares of fp32 are summed in fp32 over a few dozen elements and
-in fp64 beyond: 64 roundings of 2^-24 bound the norm's relative error by 2e-6
+in more bits beyond: 64 roundings of 2^-24 bound the norm's relative error by 2e-6
 (half of it, in fact: the root).  A clipped element is one product with a
 coefficient rounded to fp32: three roundings on top of the norm's error; one
 more of 2^-9 for bf16.  A product below the normal range of either type has its

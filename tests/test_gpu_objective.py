@@ -3,9 +3,9 @@ the fp64 oracle.
 
 Tolerances.  A token's derivative is made of one fp32 difference, exp or
 expm1 (2 ulp), and a few products: 2e-6 of its terms' magnitudes.  The loss
-adds such terms in fp64: 2e-6 of the sum of magnitudes.  The preference loss
-is computed in fp64 from exact differences and rounded: 1e-6.  dh is rounded
-to bf16 once: 2^-8 of the element."""
+adds such terms in pairs of fp32 (48 bits): 2e-6 of the sum of magnitudes.  The
+preference loss is computed in such pairs from exact differences and rounded:
+1e-6.  dh is rounded to bf16 once: 2^-8 of the element."""
 import math
 
 import numpy as np
