@@ -300,3 +300,43 @@ def test_rows_past_two_to_the_31_elements():
     policy(t, [1.0, -1.0], True, reduction=SUM, dh_nll=src, dh=dh)
     want = t.w[1:-1].to(torch.bfloat16)
     assert torch.equal(dh[:, 0], want) and torch.equal(dh[:, -1], want) and torch.equal(dh[-3:, 1000], want[-3:])
+
+
+# Calls on both sides of the number of tokens (256) and of sequences or pairs (32) up to which they are one launch.
+@pytest.mark.parametrize("lens", [[5, 0, 31, 1, 100, 64, 0], [256], [257], [8] * 32, [7] * 33, [1] * 31 + [225]])
+@pytest.mark.parametrize("reduction", [SUM, MEAN_TOKENS, MEAN_SEQS])
+@pytest.mark.parametrize("kl,per_token", [(False, True), (True, False)])
+def test_policy_few_tokens(lens, reduction, kl, per_token):
+    t = Tokens(sum(lens), lens, d=72)
+    adv = np.random.default_rng(5).standard_normal(t.T if per_token else len(t.lens))
+    check_policy(t, adv, kl, reduction=reduction)
+
+
+@pytest.mark.parametrize("lens", [[5, 0, 31, 1, 100, 64], [128, 128], [0, 257], [4] * 64, [3] * 66])
+@pytest.mark.parametrize("kind,smoothing", [(0, 0.15), (1, 0.0), (2, 0.0)])
+@pytest.mark.parametrize("mean_tokens", [False, True])
+def test_pref_few_tokens(lens, kind, smoothing, mean_tokens):
+    check_pref(Tokens(sum(lens), lens, d=72), True, kind, mean_tokens, smoothing=smoothing)
+
+
+@pytest.mark.parametrize("d", [8, 16, 248, 256, 264, 1024, 2056, 11008])
+def test_row_widths_of_many_tokens(d):
+    check_policy(Tokens(d, [7, 300], d=d), [1.0, -0.5], True)
+    check_pref(Tokens(d + 1, [290, 30], d=d))
+
+
+@pytest.mark.parametrize("off", [[0, 900, 600], [0, 300, 700], [5, 300, 600], [0, -4, 600]])
+def test_offsets_out_of_order_among_many_tokens_are_reported(off):
+    t = Tokens(9, [300, 300])
+    t.doff = torch.tensor(off, dtype=torch.int32, device="cuda")
+    pref(t, True, SIGMOID, True, 0.1, 0.0, 0.0, 1.0, status=lora.LORA_EINVAL)
+    assert (t.dh[t.T:] == 55).all() and float(t.w[0]) == 55 and float(t.w[t.T + 1]) == 55
+
+
+def test_rows_of_many_tokens_in_place():
+    """dh over dh_nll: the same bits as apart, however far ahead rows are read."""
+    t = Tokens(41, [3000, 2500], d=1032, junk=False)
+    check_policy(t, [1.0, -0.5], True)
+    t2 = Tokens(41, [3000, 2500], d=1032, junk=False)
+    policy(t2, [1.0, -0.5], True, dh=t2.dh_nll)
+    assert torch.equal(t2.dh_nll, t.dh[:t.T])
