@@ -12,7 +12,7 @@
 // Many tensors are bound by memory: a read for the norm, a read from L2 or HBM and a write for the scaling.  What the
 // sum reads last is asked to stay in L2, all else to leave first (28 layers of 16 tensors, 97 MB: 39.8 us call after
 // call, 44.9 where nothing was in L2 before; 194 MB at the copy rate take 28.7, 291 take 43).  Few tensors are bound by
-// the chain launch, load, sum, exchange, store: 4.5 us for four tensors, 0.66 MB.
+// the chain launch, load, sum, exchange, store: 4.0 us for four tensors, 0.66 MB.
 // FP64 is scarce on this GPU (about 2 operations a clock and SM), so a lane's 16 squares are summed in fp32 and these
 // sums as pairs of fp32; only the warps' sums are added in fp64.  The tensors' table is a kernel argument: no copy
 // precedes the launches.
@@ -27,7 +27,7 @@ namespace {
 
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
 constexpr int kScaleWarps = 16;  // of the scaling, one CTA per SM: their registers hold what is on its way
-constexpr int kOneCtas = 16;     // of the single cluster
+constexpr int kOneCtas = 16, kOneWarps = 16;  // of the single cluster, which holds a piece per warp
 
 // A piece's place: the elements before the first 16-byte boundary of src (head), the vectors behind them, the rest.
 struct Piece {
@@ -293,10 +293,11 @@ __device__ __forceinline__ void store_piece(const Piece& p, int lane, const Held
 }
 
 // The CTA's sum of the warps', in warp 0; one barrier.
+template <int WARPS>
 __device__ __forceinline__ double cta_sum(double v, double* part) {
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
   __syncthreads();
-  return threadIdx.x < 32 ? warp_sum(part[threadIdx.x]) : 0.0;
+  return threadIdx.x < 32 ? warp_sum(threadIdx.x < WARPS ? part[threadIdx.x] : 0.0) : 0.0;
 }
 
 // The run of pieces [c0, c1) that is this CTA's; its warps take them in turn.
@@ -338,7 +339,7 @@ __global__ void __launch_bounds__(kThreads) clip_sum_kernel(const __grid_constan
       squares.add(now, h1);
     }
   }
-  const double sum = cta_sum(warp_total(squares, b, c0 + (int)(threadIdx.x >> 5), c1), part);
+  const double sum = cta_sum<kWarps>(warp_total(squares, b, c0 + (int)(threadIdx.x >> 5), c1), part);
   if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
@@ -385,14 +386,15 @@ __global__ void __launch_bounds__(32 * kScaleWarps)
 }
 
 template <typename Table>
-__global__ void __launch_bounds__(kThreads) clip_one_kernel(const __grid_constant__ Table b, float max_norm,
-                                                            float* __restrict__ norm_out,
-                                                            float* __restrict__ coef_out) {
-  __shared__ double part[kWarps], all[kOneCtas];
+__global__ void __launch_bounds__(32 * kOneWarps)
+    clip_one_kernel(const __grid_constant__ Table b, float max_norm, float* __restrict__ norm_out,
+                    float* __restrict__ coef_out) {
+  __shared__ double part[kOneWarps], all[kOneCtas];
   __shared__ Coef s_coef;
   const int lane = threadIdx.x & 31;
   // pieces go round the CTAs, so that few of them use every SM of the cluster
   const int c = (int)(threadIdx.x >> 5) * kOneCtas + (int)blockIdx.x;
+  cluster_begun_arrive();
   griddep_wait();
   griddep_launch_dependents();
   Piece p;
@@ -405,7 +407,9 @@ __global__ void __launch_bounds__(kThreads) clip_one_kernel(const __grid_constan
     squares.add(p, h0);
     squares.add(p, h1);
   }
-  double sum = cta_sum(warp_total(squares, b, c, min(c + 1, b.chunks)), part);
+  double sum = cta_sum<kOneWarps>(warp_total(squares, b, c, min(c + 1, b.chunks)), part);
+  __syncwarp();
+  cluster_begun_wait();
   if (threadIdx.x < kOneCtas) {
     sum = __shfl_sync((1u << kOneCtas) - 1u, sum, 0);
     const uint32_t to = mapa_shared(smem_u32(&all[blockIdx.x]), threadIdx.x);
@@ -470,9 +474,9 @@ cudaError_t with_table(const ClipBatch& b, Fn fn) {
 
 }  // namespace
 
-// One launch or two (us): 16384 elements 3.6 and 4.9, 131072 4.2 and 5.1, 262144 5.3 and 5.1 (with a launch less for
-// the host), 524288 7.9 and 5.3.
-bool clip_is_small(const ClipBatch& b) { return b.chunks <= kOneCtas * kWarps / 2; }
+// One launch or two (us): 16384 elements 3.2 and 4.8, 131072 3.8 and 5.0, 245760 4.7 and 5.0; two pieces a warp, for
+// twice the elements, took longer than two launches (524288: 7.9 and 5.3).
+bool clip_is_small(const ClipBatch& b) { return b.chunks <= kOneCtas * kOneWarps; }
 
 // A quarter of a CTA's warps at work are enough to keep its loads in flight; more CTAs cost more partial sums.
 int clip_ctas(int chunks, int num_sms) {
@@ -500,7 +504,7 @@ cudaError_t launch_clip_one(const ClipBatch& b, float max_norm, float* norm, flo
     static std::atomic<unsigned long long> done{0};
     const cudaError_t e = allow_cluster_once(clip_one_kernel<T>, done);
     if (e != cudaSuccess) return e;
-    return launch_kernel(clip_one_kernel<T>, dim3(kOneCtas), dim3(kThreads), 0, st, kOneCtas, t, max_norm, norm, coef);
+    return launch_kernel(clip_one_kernel<T>, dim3(kOneCtas), dim3(32 * kOneWarps), 0, st, kOneCtas, t, max_norm, norm, coef);
   });
 }
 

@@ -46,12 +46,13 @@ __device__ __forceinline__ Totals warp_totals(Totals v) {
   return v;
 }
 
-// Every thread of the cluster gets the sums over it, added in the order of the warps: each warp's go into its slot
-// of every CTA's shared memory.
+// Every thread of the cluster gets the sums over it, added in the order of the warps: each warp's go into its slot of
+// every CTA's shared memory (after cluster_begun_arrive() where there are several).
 __device__ __forceinline__ Totals cluster_totals(Totals v, Totals* slots) {
   const uint32_t ctas = cluster_size(), rank = ctas > 1 ? cluster_ctarank() : 0;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   v = warp_totals(v);
+  if (ctas > 1) cluster_begun_wait();
   if (lane < (int)ctas) {
     const uint32_t words[6] = {__float_as_uint(v.a.hi), __float_as_uint(v.a.lo), __float_as_uint(v.b.hi),
                                __float_as_uint(v.b.lo), (uint32_t)v.n,           (uint32_t)v.m};
@@ -141,6 +142,7 @@ __device__ __forceinline__ void policy_tokens(const Objective& o, int t0, int st
 __global__ void __launch_bounds__(kThreads) policy_kernel(const __grid_constant__ Objective o) {
   __shared__ Totals slots[kMaxCluster * kWarps];
   const int ctas = (int)cluster_size(), s = (int)blockIdx.x / ctas;
+  if (ctas > 1) cluster_begun_arrive();
   griddep_wait();
   griddep_launch_dependents();
   int lo, hi;
@@ -270,6 +272,7 @@ __global__ void __launch_bounds__(kThreads) pref_kernel(const __grid_constant__ 
   __shared__ Totals slots[kMaxCluster * kWarps];
   __shared__ float s_w[2];
   const int ctas = (int)cluster_size(), p = (int)blockIdx.x / ctas, rank = (int)blockIdx.x % ctas;
+  if (ctas > 1) cluster_begun_arrive();
   griddep_wait();
   griddep_launch_dependents();
   PairTokens tokens;
