@@ -459,8 +459,10 @@ int most_clusters(int ctas) {
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
   if (set_smem_once(decode_wide_kernel<DecodeTable<8>>, kMostSmem, done) != cudaSuccess ||
-      cudaOccupancyMaxActiveClusters(&n, decode_wide_kernel<DecodeTable<8>>, &cfg) != cudaSuccess)
+      cudaOccupancyMaxActiveClusters(&n, decode_wide_kernel<DecodeTable<8>>, &cfg) != cudaSuccess) {
+    cudaGetLastError();
     return 0;
+  }
   known.store(std::max(n, 1), std::memory_order_relaxed);
   return n;
 }

@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(kThreads, kRowCtas) rows_kernel(const __grid_c
 
   const int vecs = o.dh ? o.d / 8 : 0, parts = o.dh ? (vecs + kPartVecs - 1) / kPartVecs : 1;
   const long long warps = ((long long)gridDim.x - 1) * kWarps, w0 = ((long long)blockIdx.x - 1) * kWarps + warp;
-  // The warp's i-th part; lane l holds those with i % 32 == l, of this round of 32 and the next.
+  // The warp's i-th part; lane l holds those with i % 32 == l, of these 32 and the next.
   struct Part {
     int t, part;
     bool copied;
