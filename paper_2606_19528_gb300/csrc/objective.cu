@@ -2,7 +2,7 @@
 //   policy_kernel  clipped policy loss with a KL term, one cluster of 1 or 8 CTAs per sequence
 //   pref_kernel    loss of a chosen against a rejected sequence, one cluster per pair
 //   rows_kernel    the loss's sum, the tokens' weights w_t = d loss / d nll_t, and dh_t = w_t * d nll_t / d h_t
-//   few_kernel     all of either loss for few tokens: 3.2 us for 61 of 256
+//   few_kernel     all of either loss for few tokens: 3.2 to 3.8 us for 61 of 256
 // The first launch reads a few bytes per token and is a chain of latencies (about 4.5 us with the launches); the
 // second streams two rows of d bf16 per trainable token, one per masked token, and is bound by memory: 58 us for the
 // 352 MB of 49152 tokens of 2048, a quarter of them masked, 0.9 of the copy rate.  It needs the first one's sums (a
