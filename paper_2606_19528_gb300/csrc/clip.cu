@@ -307,8 +307,8 @@ __device__ __forceinline__ void run_of(int chunks, int* c0, int* c1) {
 }
 
 template <typename Table>
-__global__ void __launch_bounds__(kThreads) clip_sum_kernel(const __grid_constant__ Table b,
-                                                            double* __restrict__ partial, float keep) {
+__global__ void __launch_bounds__(kThreads) clip_sum_kernel(const __grid_constant__ Table b, double* partial,
+                                                            float keep) {
   griddep_wait();
   griddep_launch_dependents();
   __shared__ double part[kWarps];
@@ -343,10 +343,12 @@ __global__ void __launch_bounds__(kThreads) clip_sum_kernel(const __grid_constan
   if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
+// This grid runs beside the one that writes `partial`, up to griddep_wait(): the pointer is not __restrict__, which would
+// let the compiler read it earlier, or through a cache that does not see the writes.
 template <typename Table>
 __global__ void __launch_bounds__(32 * kScaleWarps)
-    clip_scale_kernel(const __grid_constant__ Table b, const double* __restrict__ partial, int n_partial, float max_norm,
-                      float* __restrict__ norm_out, float* __restrict__ coef_out) {
+    clip_scale_kernel(const __grid_constant__ Table b, const double* partial, int n_partial, float max_norm,
+                      float* norm_out, float* coef_out) {
   __shared__ Coef s_coef;
   const int lane = threadIdx.x & 31;
   const uint64_t pass = policy_pass();
@@ -365,7 +367,7 @@ __global__ void __launch_bounds__(32 * kScaleWarps)
   griddep_launch_dependents();
   if (threadIdx.x < 32) {
     double sum = 0.0;
-    for (int k = threadIdx.x; k < n_partial; k += 32) sum += partial[k];
+    for (int k = threadIdx.x; k < n_partial; k += 32) sum += __ldcg(partial + k);
     sum = warp_sum(sum);
     if (threadIdx.x == 0) s_coef = coef_of(sum, max_norm, norm_out, coef_out, blockIdx.x == 0);
   }
@@ -387,8 +389,7 @@ __global__ void __launch_bounds__(32 * kScaleWarps)
 
 template <typename Table>
 __global__ void __launch_bounds__(32 * kOneWarps)
-    clip_one_kernel(const __grid_constant__ Table b, float max_norm, float* __restrict__ norm_out,
-                    float* __restrict__ coef_out) {
+    clip_one_kernel(const __grid_constant__ Table b, float max_norm, float* norm_out, float* coef_out) {
   __shared__ double part[kOneWarps], all[kOneCtas];
   __shared__ Coef s_coef;
   const int lane = threadIdx.x & 31;

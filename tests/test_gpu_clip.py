@@ -197,3 +197,20 @@ def test_tensor_past_two_to_the_31_elements():
     norm, coef = run([(g, g)], math.sqrt(n))
     assert norm == pytest.approx(2.0 * math.sqrt(n), rel=2e-6) and coef == pytest.approx(0.5, rel=2e-6)
     assert (g[:100] == 1).all() and (g[-100:] == 1).all() and float(g[::4096].float().sum()) == g[::4096].numel()
+
+
+@pytest.mark.parametrize("n", [300001, 3000001])
+def test_large_calls_follow_the_gradients_in_stream_order(n):
+    """Above the size of one launch, right behind the kernels that write the gradients, with the workspace of the
+    call before: each call's norm, coefficient and clipped tensor are those of its own gradients."""
+    g = torch.empty(n, device="cuda")
+    norms, coefs, outs = torch.empty(20, device="cuda"), torch.empty(20, device="cuda"), torch.empty(20, n, device="cuda")
+    arrs = [lora.make_grads([(g, out)]) for out in outs]
+    ws = G.workspace(lora.lora_clip_workspace_size(arrs[0]))
+    for i, arr in enumerate(arrs):
+        g.fill_(float(2 ** (i % 5) * (i + 1)))
+        lora.lora_clip_grads(arr, 1.0, norms[i:], coefs[i:], ws, ws.numel())
+    torch.cuda.synchronize()
+    want = torch.tensor([2 ** (i % 5) * (i + 1) for i in range(20)], device="cuda").double() * math.sqrt(n)
+    assert torch.allclose(norms.double(), want, rtol=2e-6, atol=0) and torch.allclose(coefs.double(), 1 / want, rtol=2e-6, atol=0)
+    assert ((outs.double() * math.sqrt(n) - 1).abs() <= 3e-6).all()
