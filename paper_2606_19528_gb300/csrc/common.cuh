@@ -40,8 +40,11 @@ __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
 
 // Programmatic dependent launch.  griddep_wait blocks until every grid this
 // one depends on has completed and its writes are visible (a no-op for a grid
-// launched without the attribute); every kernel calls it before its first
-// global access.  griddep_launch_dependents lets the next grid of the stream
+// launched without the attribute); every kernel calls it before its first access
+// to what the grid before may write.  That memory is not read-only for the
+// kernel's lifetime: no const __restrict__ pointer and no __ldg reads it, either
+// of which lets the compiler move a load before the wait.
+// griddep_launch_dependents lets the next grid of the stream
 // start launching (its CTAs run their prologue and then wait themselves).
 __device__ __forceinline__ void griddep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void griddep_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

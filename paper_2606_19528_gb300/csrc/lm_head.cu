@@ -38,9 +38,9 @@ constexpr int kScanThreads = 1024;
 // of a thread issued before its stores).
 constexpr int kMarkThreads = 128;
 
-__global__ void __launch_bounds__(kMarkThreads) vocab_mark_kernel(const int32_t* __restrict__ targets,
-                                                                  const uint8_t* __restrict__ mask, int T,
-                                                                  const int32_t* __restrict__ topk, long long ld,
+__global__ void __launch_bounds__(kMarkThreads) vocab_mark_kernel(const int32_t* targets,
+                                                                  const uint8_t* mask, int T,
+                                                                  const int32_t* topk, long long ld,
                                                                   int k, int V, uint8_t* __restrict__ flags,
                                                                   int32_t* __restrict__ counts) {
   griddep_wait();
@@ -127,7 +127,7 @@ __device__ int compact(int n, Flag flag, int first, int32_t* list, int32_t* inv)
 constexpr int kSegs = 128;  // vocabulary segments of the multi-block compaction
 
 // Set flags per vocabulary segment (every token in full-vocabulary mode).
-__global__ void __launch_bounds__(256) vocab_count_kernel(const uint8_t* __restrict__ flags, int V, int full,
+__global__ void __launch_bounds__(256) vocab_count_kernel(const uint8_t* flags, int V, int full,
                                                           int32_t* __restrict__ seg_counts) {
   griddep_wait();
   griddep_launch_dependents();
@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(256) vocab_count_kernel(const uint8_t* __restr
 }
 
 // Set flags (bytes 0 or 1) in [0, n), by the whole block; every thread gets the sum.
-__device__ int count_flags(const uint8_t* __restrict__ flags, int n) {
+__device__ int count_flags(const uint8_t* flags, int n) {
   const int n16 = n / 16;
   const uint4* f4 = reinterpret_cast<const uint4*>(flags);
   int c = 0;
@@ -167,10 +167,10 @@ __device__ int count_flags(const uint8_t* __restrict__ flags, int n) {
 // trainable target lies in J.  seg_counts null: each block counts the flags
 // before its segment (at most 2^20 bytes, from L2) instead of a launch of its own
 // counting the segments first.
-__global__ void __launch_bounds__(kScanThreads) compact_kernel(const uint8_t* __restrict__ flags, int V, int full,
-                                                               const int32_t* __restrict__ seg_counts,
-                                                               const uint8_t* __restrict__ mask, int T,
-                                                               const int32_t* __restrict__ targets, int32_t* J,
+__global__ void __launch_bounds__(kScanThreads) compact_kernel(const uint8_t* flags, int V, int full,
+                                                               const int32_t* seg_counts,
+                                                               const uint8_t* mask, int T,
+                                                               const int32_t* targets, int32_t* J,
                                                                int32_t* tl, int32_t* tpos, int32_t* counts) {
   griddep_wait();
   griddep_launch_dependents();
@@ -199,8 +199,8 @@ __global__ void __launch_bounds__(kScanThreads) compact_kernel(const uint8_t* __
   if (threadIdx.x == 0) counts[0] = nT;
 }
 
-__global__ void gather_rows_kernel(const __nv_bfloat16* __restrict__ src, long long ld,
-                                   const int32_t* __restrict__ idx, int n, int d, __nv_bfloat16* __restrict__ dst) {
+__global__ void gather_rows_kernel(const __nv_bfloat16* src, long long ld,
+                                   const int32_t* idx, int n, int d, __nv_bfloat16* __restrict__ dst) {
   griddep_wait();
   griddep_launch_dependents();
   const int vpr = d / 8;  // 16-byte vectors per row
@@ -209,7 +209,7 @@ __global__ void gather_rows_kernel(const __nv_bfloat16* __restrict__ src, long l
        e += (long long)gridDim.x * blockDim.x) {
     const int i = (int)(e / vpr), v = (int)(e % vpr);
     const uint4* s = reinterpret_cast<const uint4*>(src + (long long)idx[i] * ld) + v;
-    reinterpret_cast<uint4*>(dst + (long long)i * d)[v] = __ldg(s);
+    reinterpret_cast<uint4*>(dst + (long long)i * d)[v] = *s;
   }
 }
 
@@ -218,13 +218,13 @@ __global__ void gather_rows_kernel(const __nv_bfloat16* __restrict__ src, long l
 // of E in J (not when J is the whole vocabulary: E is read in place), and zeros in
 // the rows of dh and the losses outside the trainable set (not after a failed check: the call's
 // outputs stay untouched).
-__global__ void __launch_bounds__(256) prepare_rows_kernel(const __nv_bfloat16* __restrict__ h,
-                                                           const __nv_bfloat16* __restrict__ E, int d, int T, int V,
-                                                           const int32_t* __restrict__ tl,
-                                                           const int32_t* __restrict__ tpos,
-                                                           const int32_t* __restrict__ J,
-                                                           const int32_t* __restrict__ targets,
-                                                           const int32_t* __restrict__ counts,
+__global__ void __launch_bounds__(256) prepare_rows_kernel(const __nv_bfloat16* h,
+                                                           const __nv_bfloat16* E, int d, int T, int V,
+                                                           const int32_t* tl,
+                                                           const int32_t* tpos,
+                                                           const int32_t* J,
+                                                           const int32_t* targets,
+                                                           const int32_t* counts,
                                                            __nv_bfloat16* __restrict__ ht, __nv_bfloat16* __restrict__ ej,
                                                            int32_t* __restrict__ ycol, __nv_bfloat16* __restrict__ dh,
                                                            float* __restrict__ token_loss) {
@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(256) prepare_rows_kernel(const __nv_bfloat16* 
       uint4 q[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        if (v0 + u * 32 < vpr) q[u] = __ldg(s + v0 + u * 32);
+        if (v0 + u * 32 < vpr) q[u] = s[v0 + u * 32];
 #pragma unroll
       for (int u = 0; u < 4; ++u)
         if (v0 + u * 32 < vpr) o[v0 + u * 32] = q[u];
@@ -313,11 +313,11 @@ __device__ void finish_body(const float* rowloss, int nT, float* loss) {
 // + 9.8 us for 614 positions and 8648 tokens; this 17.5 us.)
 constexpr int kGradStep = 4096;  // four 16-byte loads per thread
 
-__global__ void __launch_bounds__(256) ce_rows_kernel(const float2* __restrict__ part, int ld_part, int ngroups,
-                                                      const float* __restrict__ Z, int ldz, int nJ,
-                                                      const int32_t* __restrict__ ycol, int nT, int chunk,
+__global__ void __launch_bounds__(256) ce_rows_kernel(const float2* part, int ld_part, int ngroups,
+                                                      const float* Z, int ldz, int nJ,
+                                                      const int32_t* ycol, int nT, int chunk,
                                                       __nv_bfloat16* __restrict__ G, int ldg, float* rowloss,
-                                                      const int32_t* __restrict__ tl, float* __restrict__ token_loss,
+                                                      const int32_t* tl, float* __restrict__ token_loss,
                                                       float* __restrict__ loss, int* __restrict__ done) {
   griddep_wait();
   griddep_launch_dependents();
@@ -391,7 +391,7 @@ __global__ void __launch_bounds__(256) ce_rows_kernel(const float2* __restrict__
 }
 
 // dst[idx[i], :] = src[i, :] for i < n.
-__global__ void scatter_rows_kernel(const __nv_bfloat16* __restrict__ src, const int32_t* __restrict__ idx, int n, int d,
+__global__ void scatter_rows_kernel(const __nv_bfloat16* src, const int32_t* idx, int n, int d,
                                     __nv_bfloat16* __restrict__ dst) {
   griddep_wait();
   griddep_launch_dependents();

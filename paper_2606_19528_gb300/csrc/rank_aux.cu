@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(256) transposes_kernel(const __grid_constant__
     const int vpr = r8 / 8;
     for (int e = threadIdx.x; e < rows * vpr; e += 256) {
       const int c = e / vpr, v = e % vpr;
-      *reinterpret_cast<uint4*>(tile + c * pitch + v * 8) = __ldg(reinterpret_cast<const uint4*>(src + (size_t)c * ld) + v);
+      *reinterpret_cast<uint4*>(tile + c * pitch + v * 8) = reinterpret_cast<const uint4*>(src + (size_t)c * ld)[v];
     }
   } else {
     for (int e = threadIdx.x; e < rows * r8; e += 256) {
@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(256) transposes_kernel(const __grid_constant__
   }
 }
 
-__global__ void pad_cols_kernel(const __nv_bfloat16* __restrict__ src, int rows, int r,
+__global__ void pad_cols_kernel(const __nv_bfloat16* src, int rows, int r,
                                 __nv_bfloat16* __restrict__ dst, int ld_dst) {
   griddep_wait();
   griddep_launch_dependents();

@@ -65,7 +65,7 @@ __device__ __forceinline__ float divide_bf16(float x, float n, float rn, bool fa
 constexpr int kNormWarps = 2, kNormStages = 4;
 constexpr int kNormPitch = 144;  // bytes of a staged row: 128 + 16, so that lanes reading 16 bytes of 32 rows spread
 
-__global__ void __launch_bounds__(kNormWarps * 32) row_norms_kernel(const __nv_bfloat16* __restrict__ E, int V, int d,
+__global__ void __launch_bounds__(kNormWarps * 32) row_norms_kernel(const __nv_bfloat16* E, int V, int d,
                                                                    float* __restrict__ norm) {
   griddep_wait();
   griddep_launch_dependents();
@@ -114,8 +114,8 @@ __global__ void __launch_bounds__(kNormWarps * 32) row_norms_kernel(const __nv_b
 }
 
 // En[i] = bf16(E[i] / norm[i]) (zero rows stay zero): eight 16-byte vectors per thread, all loads first.
-__global__ void __launch_bounds__(256) scale_rows_kernel(const __nv_bfloat16* __restrict__ E, int V, int d,
-                                                         const float* __restrict__ norm,
+__global__ void __launch_bounds__(256) scale_rows_kernel(const __nv_bfloat16* E, int V, int d,
+                                                         const float* norm,
                                                          __nv_bfloat16* __restrict__ En) {
   griddep_wait();
   griddep_launch_dependents();
@@ -129,8 +129,8 @@ __global__ void __launch_bounds__(256) scale_rows_kernel(const __nv_bfloat16* __
 #pragma unroll
   for (int u = 0; u < kU; ++u) {
     const long long e = e0 + 256 * u;
-    q[u] = e < total ? __ldg(src + e) : make_uint4(0u, 0u, 0u, 0u);
-    nr[u] = e < total ? __ldg(norm + e / nv) : 1.f;
+    q[u] = e < total ? src[e] : make_uint4(0u, 0u, 0u, 0u);
+    nr[u] = e < total ? norm[e / nv] : 1.f;
   }
 #pragma unroll
   for (int u = 0; u < kU; ++u) {
@@ -322,7 +322,7 @@ __device__ __forceinline__ void warp_sort(uint64_t (&v)[E]) {
 // A warp loads n <= 32 * E candidates, sorts them and writes the first k
 // indices to out through its 32 * E words of shared memory (whole lines).
 template <int E>
-__device__ void warp_sort_write(const uint2* __restrict__ c, int n, int k, int32_t* __restrict__ buf,
+__device__ void warp_sort_write(const uint2* c, int n, int k, int32_t* __restrict__ buf,
                                 int32_t* __restrict__ out) {
   const int lane = threadIdx.x & 31;
   uint64_t v[E];
@@ -495,11 +495,11 @@ __device__ float sample_threshold(SelShared& sh, const float (&f)[4], int rs) {
   return lo + (float)sh.bin * ((hi - lo) / 2048.f);
 }
 
-__device__ bool sampled_select(SelShared& sh, const float* __restrict__ s, int V, int k, int32_t* __restrict__ out) {
+__device__ bool sampled_select(SelShared& sh, const float* s, int V, int k, int32_t* __restrict__ out) {
   const float4* s4 = reinterpret_cast<const float4*>(s);
   const int n4 = V / 4;
   const int lane = threadIdx.x & 31;
-  const float4 q0 = __ldg(s4 + (int)(((long long)threadIdx.x * n4) / kSelThreads));  // evenly spread over the row
+  const float4 q0 = s4[(int)(((long long)threadIdx.x * n4) / kSelThreads)];  // evenly spread over the row
   const float sample[4] = {q0.x, q0.y, q0.z, q0.w};
   const float rk = (float)k * (float)kRowSample / (float)V;
   const float tf = sample_threshold(sh, sample, min(kRowSample, (int)ceilf(rk + 4.f * sqrtf(rk)) + 2));
@@ -559,7 +559,7 @@ __device__ bool sampled_select(SelShared& sh, const float* __restrict__ s, int V
 }
 
 // Similarity row s to table row trow.
-__device__ __forceinline__ void select_row(SelShared& sh, const float* __restrict__ s, int V, int k, long long trow,
+__device__ __forceinline__ void select_row(SelShared& sh, const float* s, int V, int k, long long trow,
                            int32_t* __restrict__ table, int* __restrict__ status) {
   if (V > kRowSampleMinV) {
     if (sampled_select(sh, s, V, k, table + trow * k)) return;
@@ -584,7 +584,7 @@ __device__ __forceinline__ void select_row(SelShared& sh, const float* __restric
     for (; j4 + 3 * kSelThreads < n4; j4 += 4 * kSelThreads) {  // four loads in flight per thread
       float4 q[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) q[u] = __ldg(s4 + j4 + u * kSelThreads);
+      for (int u = 0; u < 4; ++u) q[u] = s4[j4 + u * kSelThreads];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         count(q[u].x);
@@ -594,7 +594,7 @@ __device__ __forceinline__ void select_row(SelShared& sh, const float* __restric
       }
     }
     for (; j4 < n4; j4 += kSelThreads) {
-      const float4 q = __ldg(s4 + j4);
+      const float4 q = s4[j4];
       count(q.x);
       count(q.y);
       count(q.z);
@@ -663,9 +663,9 @@ __device__ __forceinline__ void select_row(SelShared& sh, const float* __restric
 // rows); kList: the first *n_list entries of rows are table rows whose similarities
 // are S's rows rows[i] - row0 (a short launch that usually finds none).
 template <bool kList>
-__global__ void __launch_bounds__(kSelThreads, 2) topk_select_kernel(const float* __restrict__ S, long long lds, int V,
-                                                                  int k, int row0, const int32_t* __restrict__ rows,
-                                                                  const int* __restrict__ n_list,
+__global__ void __launch_bounds__(kSelThreads, 2) topk_select_kernel(const float* S, long long lds, int V,
+                                                                  int k, int row0, const int32_t* rows,
+                                                                  const int* n_list,
                                                                   int32_t* __restrict__ table,
                                                                   int* __restrict__ status) {
   griddep_wait();
@@ -699,7 +699,7 @@ constexpr int kShortThreads = 256;
 constexpr int kShortRegs = 8;  // float4 per thread
 constexpr int kShortMaxV = 4 * kShortRegs * kShortThreads;
 
-__global__ void __launch_bounds__(kShortThreads, 4) topk_short_kernel(const float* __restrict__ S, long long lds, int V,
+__global__ void __launch_bounds__(kShortThreads, 4) topk_short_kernel(const float* S, long long lds, int V,
                                                                      int k, uint2* __restrict__ cand, int cap,
                                                                      int* __restrict__ cnt) {
   griddep_wait();
@@ -716,7 +716,7 @@ __global__ void __launch_bounds__(kShortThreads, 4) topk_short_kernel(const floa
 #pragma unroll
   for (int u = 0; u < kShortRegs; ++u) {
     const int j4 = tid + u * kShortThreads;
-    v[u] = j4 < n4 ? __ldg(s4 + j4) : make_float4(0.f, 0.f, 0.f, 0.f);
+    v[u] = j4 < n4 ? s4[j4] : make_float4(0.f, 0.f, 0.f, 0.f);
   }
   // f(value, index) over this thread's values
   auto each = [&](auto f) {
@@ -823,7 +823,7 @@ constexpr int kSampleRank = 56;
 constexpr int kTauThreads = 256;
 
 template <int kTauPer>  // values per thread: ns <= kTauPer * kTauThreads
-__global__ void __launch_bounds__(kTauThreads, kTauPer > 16 ? 4 : 6) topk_tau_kernel(const float* __restrict__ Z, int V, int k, int ns,
+__global__ void __launch_bounds__(kTauThreads, kTauPer > 16 ? 4 : 6) topk_tau_kernel(const float* Z, int V, int k, int ns,
                                                                 float* __restrict__ tau) {
   griddep_wait();
   griddep_launch_dependents();
@@ -928,7 +928,7 @@ constexpr int kWarpSortMax = 1024;
 constexpr int kSortThreads = 256;
 
 __global__ void __launch_bounds__(kSortThreads, 2) topk_sort_warp_kernel(
-    const uint2* __restrict__ cand, const int* __restrict__ cnt, int cap, int k, int row0, int nrows,
+    const uint2* cand, const int* cnt, int cap, int k, int row0, int nrows,
     int32_t* __restrict__ table, int32_t* __restrict__ big_rows, int* __restrict__ big_count,
     int32_t* __restrict__ fail_rows, int* __restrict__ fail_count) {
   griddep_wait();
@@ -960,10 +960,10 @@ __global__ void __launch_bounds__(kSortThreads, 2) topk_sort_warp_kernel(
 
 // The rows the warp sort listed (more than 1024 candidates): one block of 256
 // threads per row (up to 16 register slots each), rows taken from the list.
-__global__ void __launch_bounds__(kSortThreads, 4) topk_sort_kernel(const uint2* __restrict__ cand,
-                                                                   const int* __restrict__ cnt, int cap, int k,
-                                                                   int row0, const int32_t* __restrict__ big_rows,
-                                                                   const int* __restrict__ big_count,
+__global__ void __launch_bounds__(kSortThreads, 4) topk_sort_kernel(const uint2* cand,
+                                                                   const int* cnt, int cap, int k,
+                                                                   int row0, const int32_t* big_rows,
+                                                                   const int* big_count,
                                                                    int32_t* __restrict__ table) {
   griddep_wait();
   griddep_launch_dependents();
@@ -984,7 +984,7 @@ __global__ void __launch_bounds__(kSortThreads, 4) topk_sort_kernel(const uint2*
 }
 
 // Es[i, :] = En[floor(i * V / ns), :] for i < ns: the sample tokens, evenly spread.
-__global__ void topk_gather_sample_kernel(const __nv_bfloat16* __restrict__ En, int V, int d, int ns,
+__global__ void topk_gather_sample_kernel(const __nv_bfloat16* En, int V, int d, int ns,
                                           __nv_bfloat16* __restrict__ Es) {
   griddep_wait();
   griddep_launch_dependents();
