@@ -127,7 +127,8 @@ struct Step {
 // every warps-th 16 of the adapter's columns.  A step's weights are loaded while the one before is computed; loading
 // two to four steps ahead takes the registers of as many warps and is slower.  A lane's word of 8 codes makes the
 // fragments of two MMAs, whose k index is then a permutation of the columns; the activation's fragments share it: 16
-// consecutive bytes of token g, which come through L1.
+// consecutive bytes of token g, which come through L1.  Activations and adapters are read by plain loads, since a launch
+// that this one overlaps may have written them; codes and parameters, which do not change, are not.
 //
 // OWN: each block computes su of its projection beside y, from all of A, in the same loop: 16 adapter rows are one more
 // tile, whose fragments come from A as they lie; no launch goes before.
@@ -168,9 +169,9 @@ __global__ void __launch_bounds__(kMostThreads) decode_kernel(const __grid_const
       a[e] = 0u;
       if (n < p.N && j < r) {
         if (r % 2 == 0)
-          a[e] = __ldg(reinterpret_cast<const uint32_t*>(q));
+          a[e] = *reinterpret_cast<const uint32_t*>(q);
         else
-          a[e] = __ldg(q) | (j + 1 < r ? (uint32_t)__ldg(q + 1) << 16 : 0u);
+          a[e] = q[0] | (j + 1 < r ? (uint32_t)q[1] << 16 : 0u);
       }
     }
   };
@@ -197,13 +198,13 @@ __global__ void __launch_bounds__(kMostThreads) decode_kernel(const __grid_const
 #pragma unroll
     for (int m = 0; m < NT; ++m)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) xv[m][q] = in ? __ldg(x4[m] + c * (kChunk / 8) + q) : make_uint4(0u, 0u, 0u, 0u);
+      for (int q = 0; q < 4; ++q) xv[m][q] = in ? x4[m][c * (kChunk / 8) + q] : make_uint4(0u, 0u, 0u, 0u);
     uint4 av[OWN ? 4 : 1][2];
     if (OWN && r)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        av[q][0] = in ? __ldg(a0 + c * (kChunk / 8) + q) : make_uint4(0u, 0u, 0u, 0u);
-        av[q][1] = in && r > 8 ? __ldg(a1 + c * (kChunk / 8) + q) : make_uint4(0u, 0u, 0u, 0u);
+        av[q][0] = in ? a0[c * (kChunk / 8) + q] : make_uint4(0u, 0u, 0u, 0u);
+        av[q][1] = in && r > 8 ? a1[c * (kChunk / 8) + q] : make_uint4(0u, 0u, 0u, 0u);
       }
     fetch(s, c + warps);
     if (OWN && r)

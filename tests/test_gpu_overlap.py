@@ -91,3 +91,57 @@ def test_training_steps_with_new_adapters(T, r):
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert all(torch.equal(a[k], b[k]) for k in b)
+
+
+class Decode:
+    """A projection with 4-bit weights for T tokens."""
+
+    def __init__(self, g, T, K, N, r, x=None):
+        self.T, self.K, self.N, self.r = T, K, N, r
+        s = torch.empty(N, K // 64, device="cuda").uniform_(0.2, 0.45, generator=g) * K ** -0.5
+        self.params = torch.stack([s, -7.5 * s], dim=-1).to(torch.bfloat16).contiguous()
+        self.codes = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+        self.A = rand(g, r, K, std=K ** -0.5) if r else None
+        self.B = rand(g, N, r, std=0.1) if r else None
+        self.x = torch.zeros(T, K, dtype=torch.bfloat16, device="cuda") if x is None else x
+        self.y = torch.zeros(T, N, dtype=torch.bfloat16, device="cuda")
+
+    def projs(self, x=None, y=None):
+        return lora.make_projs([lora.make_proj(lora.make_shape(self.T, self.K, self.N, self.r, 2.0),
+                                               x=self.x if x is None else x, A=self.A, B=self.B,
+                                               y=self.y if y is None else y, Wq=lora.make_q4(self.codes, self.params))])
+
+
+@pytest.mark.parametrize("T,K,N,r", [(1, 256, 256, 8), (5, 512, 512, 0), (3, 512, 512, 32), (16, 1024, 1024, 0),
+                                     (16, 3072, 30000, 0), (9, 3072, 30000, 16)])
+def test_decode_of_what_the_call_before_wrote(T, K, N, r):
+    """Three projections in a row, each of the last one's output; without adapters and as one launch the blocks' first
+    loads come right behind the wait."""
+    g = torch.Generator(device="cuda").manual_seed(T + K + N)
+    first = Decode(g, T, K, K, r)
+    second = Decode(g, T, K, K, r, first.y)
+    third = Decode(g, T, K, N, r, second.y)
+    chain = (first, second, third)
+    calls = [p.projs() for p in chain]
+    n = max(lora.lora_decode_workspace_size(c) for c in calls)
+    ws = G.workspace(n)
+    xs = [rand(g, T, K) for _ in range(8)]
+    want = []
+    for x in xs:
+        outs = []
+        for p in chain:
+            y = torch.zeros_like(p.y)
+            lora.lora_decode_q4(p.projs(x, y), G.workspace(n), max(n, 256))
+            torch.cuda.synchronize()
+            outs.append(y)
+            x = y
+        want.append(outs)
+    got = []
+    for x in xs:
+        first.x.copy_(x)
+        for c in calls:
+            lora.lora_decode_q4(c, ws, ws.numel())
+        got.append([p.y.clone() for p in chain])
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert all(torch.equal(x, y) for x, y in zip(a, b)) and not torch.equal(a[-1], torch.zeros_like(a[-1]))
