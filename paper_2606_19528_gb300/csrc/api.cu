@@ -2204,7 +2204,8 @@ int clip_batches(const lora_grad* grads, int n, int* partials, Launch launch) {
 // policy), 47.0 with 40 MB, 44.9 with 60, 44.4 with 80; the same 97 MB call after call 43.0, 40.8, 39.8 and 41.1.
 constexpr double kClipKeepBytes = 60e6;
 
-int clip_check(const lora_grad* grads, int n, size_t* bytes) {
+// *batches: of the launches of the call.
+int clip_check(const lora_grad* grads, int n, size_t* bytes, int* batches) {
   if (!grads) return LORA_ENULL;
   if (n < 1 || n > 65536) return LORA_EINVAL;
   for (int i = 0; i < n; ++i) {
@@ -2212,7 +2213,11 @@ int clip_check(const lora_grad* grads, int n, size_t* bytes) {
     if (g.n < 0 || g.n > (1ll << 38) || (g.dtype != LORA_F32 && g.dtype != LORA_BF16)) return LORA_EINVAL;
   }
   int partials = 0;
-  clip_batches(grads, n, &partials, [](const ClipBatch&, int, int) { return LORA_OK; });
+  *batches = 0;
+  clip_batches(grads, n, &partials, [&](const ClipBatch&, int, int) {
+    ++*batches;
+    return LORA_OK;
+  });
   *bytes = up256((size_t)partials * sizeof(double)) + 256;
   return LORA_OK;
 }
@@ -2827,13 +2832,15 @@ int lora_pref_fwd_bwd(const lora_pref_args* a, void* workspace, size_t workspace
 
 int lora_clip_workspace_size(const lora_grad* grads, int n_grads, size_t* bytes) {
   if (!bytes) return rec(LORA_ENULL);
-  return rec(clip_check(grads, n_grads, bytes));
+  int batches = 0;
+  return rec(clip_check(grads, n_grads, bytes, &batches));
 }
 
 int lora_clip_grads(const lora_grad* grads, int n_grads, float max_norm, float* norm, float* coef, void* workspace,
                     size_t workspace_bytes, void* stream) {
   size_t need = 0;
-  int rc = clip_check(grads, n_grads, &need);
+  int batches = 0;
+  int rc = clip_check(grads, n_grads, &need, &batches);
   if (rc != LORA_OK) return rec(rc);
   if (!(max_norm >= 0.f)) return rec(LORA_EINVAL);
   if (!norm) return rec(LORA_ENULL);
@@ -2845,13 +2852,12 @@ int lora_clip_grads(const lora_grad* grads, int n_grads, float max_norm, float* 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   double* partial = at<double>(workspace, 0);
   int partials = 0, again = 0;
-  const bool one_batch = n_grads <= kClipTensors;
   bool done = false;
   double total = 1.0;
   for (int i = 0; i < n_grads; ++i) total += (double)grads[i].n * (grads[i].dtype == LORA_BF16 ? 2 : 4);
   const float keep = (float)std::min(1.0, kClipKeepBytes / total);
   rc = clip_batches(grads, n_grads, &partials, [&](const ClipBatch& b, int first, int ctas) {
-    done = one_batch && clip_is_small(b);
+    done = batches == 1 && clip_is_small(b);
     return (done ? launch_clip_one(b, max_norm, norm, coef, st) : launch_clip_sum(b, partial + first, ctas, keep, st)) ==
                    cudaSuccess
                ? LORA_OK

@@ -214,3 +214,16 @@ def test_large_calls_follow_the_gradients_in_stream_order(n):
     want = torch.tensor([2 ** (i % 5) * (i + 1) for i in range(20)], device="cuda").double() * math.sqrt(n)
     assert torch.allclose(norms.double(), want, rtol=2e-6, atol=0) and torch.allclose(coefs.double(), 1 / want, rtol=2e-6, atol=0)
     assert ((outs.double() * math.sqrt(n) - 1).abs() <= 3e-6).all()
+
+
+def test_pieces_past_one_launch_table():
+    """2^40 elements listed (one tensor of 2^31, counted 513 times) and a small tensor behind them, which begins a
+    second table: its norm is not the call's."""
+    n = 1 << 31
+    big = torch.full((n,), 2.0 ** -10, dtype=torch.bfloat16, device="cuda")
+    small = torch.arange(1.0, 101.0, device="cuda")
+    out = torch.full_like(small, NAN)
+    norm, coef = run([(big, None)] * 513 + [(small, out)], 0.5)
+    want = math.sqrt(513 * n * 2.0 ** -20 + float((small.double() ** 2).sum()))
+    assert norm == pytest.approx(want, rel=2e-6) and coef == pytest.approx(0.5 / want, rel=2e-6)
+    assert ((out.double() - small.double() * 0.5 / want).abs() <= 3e-6 * small.double()).all()
