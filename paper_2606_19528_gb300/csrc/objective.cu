@@ -125,7 +125,7 @@ __device__ __forceinline__ void policy_tokens(const Objective& o, int t0, int st
       l = -A * (up ? 1.f + o.clip_high : 1.f - o.clip_low);
       ++v.m;
     } else {
-      u[k] = A * expf(delta);
+      u[k] = A == 0.f && isfinite(delta) ? 0.f : A * expf(delta);  // also where the exponential is beyond fp32
       l = -u[k];
     }
     if (o.ref_nll) {

@@ -340,3 +340,24 @@ def test_rows_of_many_tokens_in_place():
     t2 = Tokens(41, [3000, 2500], d=1032, junk=False)
     policy(t2, [1.0, -0.5], True, dh=t2.dh_nll)
     assert torch.equal(t2.dh_nll, t.dh[:t.T])
+
+
+@pytest.mark.parametrize("lens", [[3, 4], [3, 400]])
+@pytest.mark.parametrize("per_token", [False, True])
+def test_policy_advantage_zero_with_a_ratio_beyond_fp32(lens, per_token):
+    """0 * rho is 0 for every finite rho = exp(delta): exp(89) is 4e38."""
+    t = Tokens(60, lens, masked=False, junk=False)
+    t.nll[0], t.old[0] = 1.0, 90.0
+    t.nll[1], t.old[1] = 0.5, 700.0
+    for k in ("nll", "old"):
+        t.dev[k] = f32(getattr(t, k))
+    adv = np.where(np.arange(t.T) < 3, 0.0, 0.5) if per_token else [0.0, 0.5]
+    for reduction in (SUM, MEAN_TOKENS, MEAN_SEQS):
+        policy(t, adv, False, reduction=reduction, scale=1.3)
+        loss, w, _, _ = oracle.policy_loss(t.nll, t.old, None, np.asarray(adv, np.float32), t.mask, t.off,
+                                           float(np.float32(0.2)), 0.25, 0.0, float(np.float32(1.3)), reduction)
+        assert w[0] == 0 and w[1] == 0 and math.isfinite(loss)
+        assert np.allclose(t.w[1:-1].double().cpu().numpy(), w, rtol=2e-6, atol=0)
+        # the terms left are A rho of one sign: their sum is the sum of their magnitudes
+        assert float(t.loss[0]) == pytest.approx(loss, rel=2e-6)
+        t.check_rows(w)
