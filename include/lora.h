@@ -334,8 +334,9 @@ enum {
  * delta > log(1 + clip_high), or A < 0 and delta < log(1 - clip_low), the fp32
  * difference against the fp32 logarithm.  exp(e) - 1 - e >= 0 estimates the
  * divergence of the model from the reference on a sampled token; ref_nll NULL:
- * no such term.  stats[0] receives its mean over the trainable tokens, stats[1]
- * the share of them that is clipped (0 without any).
+ * no such term; beta 0: it is no part of the loss, whatever its values, and
+ * stats has it all the same.  stats[0] receives its mean over the trainable
+ * tokens, stats[1] the share of them that is clipped (0 without any).
  * 0 <= clip_low <= 1, 0 <= clip_high; clip_high, beta and scale finite. */
 typedef struct lora_policy_args {
   int64_t T, S, d;

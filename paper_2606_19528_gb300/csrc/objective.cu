@@ -131,7 +131,7 @@ __device__ __forceinline__ void policy_tokens(const Objective& o, int t0, int st
     if (o.ref_nll) {
       const float e = nll[k] - ref[k], kl = exp_minus_line(e);
       v.b.add(kl);
-      u[k] = fmaf(o.beta, expm1f(e), u[k]);
+      if (o.beta != 0.f) u[k] = fmaf(o.beta, expm1f(e), u[k]);
     }
     v.a.add(l);
     ++v.n;
@@ -306,7 +306,7 @@ __device__ void finish(const Objective& o) {
       const int tokens = o.n[s];
       Pair l, k;
       l.hi = q.loss_hi, l.lo = q.loss_lo, k.hi = q.kl_hi, k.lo = q.kl_lo;
-      if (o.policy && o.ref_nll) l.add(k.times(o.beta));
+      if (o.policy && o.ref_nll && o.beta != 0.f) l.add(k.times(o.beta));
       loss.add(by_seq && tokens ? l.over((float)tokens) : l);
       kl.add(k);
       n += tokens;

@@ -361,3 +361,19 @@ def test_policy_advantage_zero_with_a_ratio_beyond_fp32(lens, per_token):
         # the terms left are A rho of one sign: their sum is the sum of their magnitudes
         assert float(t.loss[0]) == pytest.approx(loss, rel=2e-6)
         t.check_rows(w)
+
+
+@pytest.mark.parametrize("lens", [[3, 4], [3, 400]])
+@pytest.mark.parametrize("reduction", [SUM, MEAN_TOKENS, MEAN_SEQS])
+def test_policy_beta_zero_with_a_divergence_beyond_fp32(lens, reduction):
+    """beta 0 with a reference model, for the statistics alone: loss and weights are those without one, to the bit."""
+    t = Tokens(61, lens, masked=False, junk=False)
+    t.nll[0], t.old[0], t.ref[0] = 97.0, 97.0, 1.0
+    for k in ("nll", "old", "ref"):
+        t.dev[k] = f32(getattr(t, k))
+    policy(t, [0.7, -0.5], False, beta=0.0, reduction=reduction)
+    want = [v.clone() for v in (t.loss[:1], t.w, t.dh)]
+    assert torch.isfinite(t.loss[0])
+    stats = policy(t, [0.7, -0.5], True, beta=0.0, reduction=reduction)
+    assert all(torch.equal(a, b) for a, b in zip(want, (t.loss[:1], t.w, t.dh)))
+    assert stats[0] == math.inf  # exp(96) / 403 is 1e39
