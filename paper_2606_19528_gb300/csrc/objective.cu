@@ -244,11 +244,12 @@ __device__ __forceinline__ void pref_pair(const Objective& o, int p, const Total
     loss.add(log1pf(e));
     slope = o.beta * (mv < 0.f ? fmaf(ls, small, (ls - 1.f) * large) : fmaf(ls, large, (ls - 1.f) * small));
   } else if (o.kind == LORA_PREF_HINGE) {
-    if (!(mv >= 1.f)) {  // also undefined
+    const float past = (mv - 1.f) + m.lo;  // m - 1; the sign also where m rounds to 1
+    if (!(past >= 0.f)) {  // also undefined
       loss = m.times(-1.f);
       loss.add(1.f);
     }
-    slope = mv < 1.f ? -o.beta : (mv >= 1.f ? 0.f : mv);
+    slope = past < 0.f ? -o.beta : (past >= 0.f ? 0.f : mv);
   } else {
     Pair x = m;
     x.add(-0.5f);

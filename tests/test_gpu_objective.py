@@ -377,3 +377,17 @@ def test_policy_beta_zero_with_a_divergence_beyond_fp32(lens, reduction):
     stats = policy(t, [0.7, -0.5], True, beta=0.0, reduction=reduction)
     assert all(torch.equal(a, b) for a, b in zip(want, (t.loss[:1], t.w, t.dh)))
     assert stats[0] == math.inf  # exp(96) / 403 is 1e39
+
+
+@pytest.mark.parametrize("lens", [[2, 1], [300, 1]])
+@pytest.mark.parametrize("off", [-1, 0, 1])
+def test_pref_hinge_beside_its_corner(lens, off):
+    """m = 1 + off 2^-40, exact in the sums' pairs of fp32 and 1 in fp32: below 1 the loss has a slope."""
+    t = Tokens(62, lens, d=16, masked=False, junk=False)
+    t.nll[:] = 0.0
+    t.ref[:] = 0.0
+    t.ref[0], t.ref[1] = 1.0, off * 2.0 ** -40
+    for k in ("nll", "ref"):
+        t.dev[k] = f32(getattr(t, k))
+    check_pref(t, kind=1, beta=1.0, margin=0.0, scale=1.0)
+    assert float(t.w[1]) == (1.0 if off < 0 else 0.0)  # d loss / d nll of the preferred answer
