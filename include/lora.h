@@ -305,7 +305,7 @@ int lora_decode_q4(const lora_proj* projs, int n_proj, void* workspace, size_t w
  * rows d nll_t / d h_t that lora_ce_fwd_bwd writes into its dh,
  *     dh_t = (d loss / d nll_t) * dh_nll_t,
  * rounded to bf16 once; rows of derivative zero are zero, whatever dh_nll
- * holds there (it is not read).  T tokens lie flat, sequence by sequence:
+ * holds there.  T tokens lie flat, sequence by sequence:
  * sequence i is [offsets[i], offsets[i+1]); offsets ascend from 0 to T
  * (checked on the device: lora_read_status then reports LORA_EINVAL and the
  * outputs are unspecified); a sequence may be empty.  Tokens with mask 0 take no

@@ -365,9 +365,8 @@ __device__ __forceinline__ long long count_tokens(const Objective& o) {
 constexpr int kVecs = 4;               // 16-byte vectors of a lane
 constexpr int kPartVecs = 32 * kVecs;  // of a part
 
-// A lane's vectors of a part times w, the token's weight (u without the norm); a row of weight zero is zero whatever it
-// holds.
-__device__ __forceinline__ void store_part(const Objective& o, int t, int part, int vecs, float u, float w,
+// A lane's vectors of a part times w, the token's weight; a row of weight zero is zero whatever it holds.
+__device__ __forceinline__ void store_part(const Objective& o, int t, int part, int vecs, float w,
                                            const uint4 (&q)[kVecs]) {
   uint4* dst = reinterpret_cast<uint4*>(o.dh + (long long)t * o.d);
 #pragma unroll
@@ -375,7 +374,7 @@ __device__ __forceinline__ void store_part(const Objective& o, int t, int part, 
     const int v = (part * kVecs + k) * 32 + (int)(threadIdx.x & 31);
     if (v >= vecs) continue;
     uint4 out = make_uint4(0u, 0u, 0u, 0u);
-    if (u != 0.f) {
+    if (w != 0.f) {
       const uint32_t in[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
       uint32_t x[4];
 #pragma unroll
@@ -460,7 +459,7 @@ __global__ void __launch_bounds__(kThreads, kRowCtas) rows_kernel(const __grid_c
     if (o.dh) nxt.copied = nxt.u != 0.f;
     for (int k = 0; k < 32; ++k) {
       const int t = __shfl_sync(0xffffffffu, cur.t, k), part = __shfl_sync(0xffffffffu, cur.part, k);
-      const float u = __shfl_sync(0xffffffffu, cur.u, k), w = u * inv;
+      const float w = __shfl_sync(0xffffffffu, cur.u, k) * inv;
       const bool copied = __shfl_sync(0xffffffffu, (int)cur.copied, k);
       more = t < o.T;
       if (!more) break;
@@ -484,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, kRowCtas) rows_kernel(const __grid_c
       const bool refill = lane == ((k + kSlots) & 31) && (k + kSlots < 32 ? cur : nxt).copied;
       if (refill) copy(k + kSlots < 32 ? cur : nxt, slot);
       if (__any_sync(0xffffffffu, refill)) pending |= 1u << slot;
-      store_part(o, t, part, vecs, u, w, r);
+      store_part(o, t, part, vecs, w, r);
       if (++slot == kSlots) slot = 0;
     }
     if (more) cur = nxt;
@@ -575,7 +574,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) few_kernel(const __grid_consta
     if (o.token_weight && part == 0 && lane == 0) o.token_weight[t] = w;
     if (!o.dh) continue;
     if (u != 0.f && !(ahead && i == w0)) fetch(t, part);
-    store_part(o, t, part, vecs, u, w, q);
+    store_part(o, t, part, vecs, w, q);
   }
 }
 

@@ -391,3 +391,16 @@ def test_pref_hinge_beside_its_corner(lens, off):
         t.dev[k] = f32(getattr(t, k))
     check_pref(t, kind=1, beta=1.0, margin=0.0, scale=1.0)
     assert float(t.w[1]) == (1.0 if off < 0 else 0.0)  # d loss / d nll of the preferred answer
+
+
+@pytest.mark.parametrize("lens", [[40], [400, 3]])
+@pytest.mark.parametrize("reduction", [MEAN_TOKENS, MEAN_SEQS])
+def test_rows_whose_weight_rounds_to_zero(lens, reduction):
+    """exp(-103) is fp32's smallest number; over 40 tokens and more it is a weight of zero, and its row is zeros."""
+    t = Tokens(63, lens, masked=False, junk=False)
+    t.nll[2], t.old[2] = 104.0, 1.0
+    for k in ("nll", "old"):
+        t.dev[k] = f32(getattr(t, k))
+    t.dh_nll[2] = float("inf")
+    policy(t, [1.0] * len(lens), False, reduction=reduction, scale=1.0)
+    assert t.w[3] == 0 and (t.dh[2] == 0).all() and torch.isfinite(t.dh).all()
