@@ -403,9 +403,11 @@ int lora_pref_fwd_bwd(const lora_pref_args* args, void* workspace, size_t worksp
  * in fp32 over a few dozen elements and in more bits from there on, from scaled
  * elements where fp32 would overflow or lose small ones, in an order that
  * depends on the tensors' sizes and alignment only.  norm (device, [1])
- * and coef (device, [1], or NULL) are written.  A norm that is not finite (a
+ * and coef (device, [1], or NULL) are written.  A sum that is not finite (a
  * gradient holds an infinity or a NaN) makes coef 1: the gradients are passed
- * on as they are, and the caller sees the norm.  max_norm >= 0, infinity for
+ * on as they are, and the caller sees the norm.  A norm of finite gradients
+ * beyond fp32 is written as infinity too; coef and dst are those of its value
+ * (coef is 1 exactly where nothing was scaled).  max_norm >= 0, infinity for
  * the norm alone.  n = 0 is allowed (src and dst may be NULL then).
  * The table of tensors is read during the call. */
 enum { LORA_F32 = 0, LORA_BF16 = 1 };
