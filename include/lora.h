@@ -286,9 +286,11 @@ int lora_topk_table(const lora_bf16* E, int64_t V, int64_t d, int64_t k, int32_t
  * weights for 1 to 16 tokens each, e.g. the q, k and v projections of a layer
  * while an answer is sampled token by token:
  *     y = x W^T + (scale x A^T) B^T,   W[n, k] = bf16(s q + b) as lora_q4_weight
- * The weights are those the training calls use, element for element.  Sums are
- * held in fp32; scale x A^T is not rounded to bf16 here (lora_linear_fwd_q4
- * does, since its backward reads it), and y is rounded once.  s must be below
+ * The weights are those the training calls use, element for element, where they
+ * are 2^-86 or more in magnitude, or zero.  Sums are held in fp32; scale x A^T is
+ * not rounded to bf16 here (lora_linear_fwd_q4 does, since its backward reads
+ * it), and y is rounded once.  Weights and sums are carried times 2^-40: smaller
+ * weights, and products below 2^-86, lose bits or vanish, and s must be below
  * 2^35 in magnitude (beyond, the weights come out infinite).
  * Fields read: shape, x, A, B, y, Wq (the others are ignored, but W must be
  * NULL).  Beyond the shapes of the other calls: T is 1 .. 16 and may differ

@@ -296,3 +296,131 @@ def test_codes_past_two_to_the_32_bytes():
     assert (y[:, :-last] == 0).all()
     p.y.copy_(y[:, -last:])
     p.check()
+
+
+class Fp32:
+    """A projection of any size, its y between guards, against fp32 products (the bound of the module's head, twice the
+    sums' part)."""
+
+    def __init__(self, g, T, K, N, r, x, s=2.0, w_scale=1.0):
+        self.T, self.K, self.N, self.r, self.s, self.x = T, K, N, r, s, x
+        sd = K ** -0.5 * w_scale
+        sc = torch.empty(N, K // 64, device="cuda").uniform_(0.2, 0.45, generator=g) * sd
+        self.codes = torch.randint(0, 256, (N, K // 2), generator=g, device="cuda", dtype=torch.uint8)
+        self.params = torch.stack([sc, -7.5 * sc], dim=-1).to(torch.bfloat16).contiguous()
+        self.A = (torch.randn(r, K, generator=g, device="cuda") * sd).to(torch.bfloat16) if r else None
+        self.B = (torch.randn(N, r, generator=g, device="cuda") * 0.1).to(torch.bfloat16) if r else None
+        self.out = torch.full((GUARD + T * N + GUARD,), 77.0, dtype=torch.bfloat16, device="cuda")
+
+    def proj(self):
+        return lora.make_proj(lora.make_shape(self.T, self.K, self.N, self.r, self.s), x=self.x, A=self.A, B=self.B,
+                              y=self.out[GUARD:], Wq=lora.make_q4(self.codes, self.params))
+
+    def y(self):
+        return self.out[GUARD:GUARD + self.T * self.N].view(self.T, self.N)
+
+    def weight(self):
+        shift = torch.tensor([[0, 16], [4, 20], [8, 24], [12, 28]], device="cuda", dtype=torch.int32)
+        q = ((self.codes.view(torch.int32)[:, :, None, None] >> shift) & 15).float().view(self.N, self.K // 64, 64)
+        p = self.params.float()
+        return (p[:, :, :1] * q + p[:, :, 1:]).to(torch.bfloat16).float().view(self.N, self.K)
+
+    def check(self):
+        x, W = self.x.float(), self.weight()
+        want, size = x @ W.T, x.abs() @ W.abs().T
+        if self.r:
+            A, B = self.A.float(), self.B.float()
+            want = want + self.s * (x @ A.T) @ B.T
+            size = size + abs(self.s) * (x.abs() @ A.abs().T) @ B.abs().T
+        y = self.y().float()
+        assert ((y - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -19 * size).all()
+        assert (self.out[:GUARD] == 77).all() and (self.out[GUARD + self.T * self.N:] == 77).all()
+
+
+@pytest.mark.parametrize("shapes", [
+    # (T, K, N, r, activation): two launches for many rows on activations of their own, narrow projections between them
+    [(2, 512, 100, 3, 0), (16, 3072, 30000, 0, 1), (5, 2048, 515, 64, 2), (9, 8192, 3000, 16, 3), (16, 3072, 20000, 13, 1),
+     (1, 64, 48, 16, 4), (16, 3072, 40, 0, 5)],
+    [(9, 3072, 30000, 16, 0), (16, 8192, 9000, 8, 1), (16, 4160, 257, 128, 2)],
+    # without adapters, no launch goes before
+    [(16, 3072, 30000, 0, 0), (3, 512, 1000, 0, 1), (9, 8192, 9000, 0, 2), (16, 1024, 40001, 0, 3)],
+    # wide ones alone, the second with the only adapter
+    [(16, 3072, 30000, 0, 0), (12, 3072, 30000, 64, 1)],
+])
+def test_kinds_of_launches_together(shapes):
+    """Calls whose projections take several launches after su's, listed in any order, on inputs that change from call to
+    call, nothing waiting between; the workspace holds NaN before the first."""
+    g = torch.Generator(device="cuda").manual_seed(len(shapes))
+    xs = {}
+    for T, K, N, r, i in shapes:
+        xs.setdefault(i, torch.zeros(T, K, dtype=torch.bfloat16, device="cuda"))
+    ps = [Fp32(g, T, K, N, r, xs[i]) for T, K, N, r, i in shapes]
+    projs = lora.make_projs([p.proj() for p in ps])
+    n = lora.lora_decode_workspace_size(projs)
+    ws = torch.full((n + 256,), 0xff, dtype=torch.uint8, device="cuda")
+    last = None
+    for seed in range(4):
+        new = [torch.randn(x.shape, generator=g, device="cuda").to(torch.bfloat16) for x in xs.values()]
+        for x, v in zip(xs.values(), new):
+            x.copy_(v)
+        for p in ps:
+            p.out[GUARD:-GUARD] = float("nan")
+        for _ in range(3):
+            lora.lora_decode_q4(projs, ws, n)
+        for p in ps:
+            p.check()
+        now = [p.y().clone() for p in ps]
+        lora.lora_decode_q4(projs, ws, n)
+        assert all(torch.equal(a, p.y()) for a, p in zip(now, ps))
+        assert last is None or not any(torch.equal(a, b) for a, b in zip(last, now))
+        last = now
+    assert (ws[n:] == 0xff).all() and lora.lora_read_status() == lora.LORA_OK
+
+
+@pytest.mark.parametrize("T,K,sizes", [(16, 3072, [(4000, 0)] * 9), (9, 2048, [(3000 + 129 * i, 4 * (i % 3)) for i in range(20)]),
+                                       (16, 1024, [(1000 + i, 16) for i in range(64)])])
+def test_many_rows_of_more_than_eight_projections(T, K, sizes):
+    """The launch for many rows with the larger of its tables."""
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn(T, K, generator=g, device="cuda").to(torch.bfloat16)
+    ps = [Fp32(g, T, K, N, r, x) for N, r in sizes]
+    projs = lora.make_projs([p.proj() for p in ps])
+    n = lora.lora_decode_workspace_size(projs)
+    ws = torch.full((n + 256,), 0xff, dtype=torch.uint8, device="cuda")
+    for _ in range(2):
+        lora.lora_decode_q4(projs, ws, n)
+    for p in ps:
+        p.check()
+    assert (ws[n:] == 0xff).all() and lora.lora_read_status() == lora.LORA_OK
+
+
+@pytest.mark.parametrize("T", [1, 5, 8])
+def test_one_launch_with_and_without_adapters(T):
+    """Ranks 16, 0, 3 and 0 in the launch that computes su itself."""
+    ps = [Proj(400 + i, T, 512, N, r) for i, (N, r) in enumerate([(300, 16), (90, 0), (17, 3), (33, 0)])]
+    run(ps)
+    for p in ps:
+        p.check()
+
+
+@pytest.mark.parametrize("K,N", [(256, 64), (2048, 40000)])
+def test_small_weights_are_those_of_the_training_forward(K, N):
+    """Weights down to 2^-86, where both launches' scaled form still holds every bit: one-hot activations read them
+    out."""
+    T = 16
+    g = torch.Generator(device="cuda").manual_seed(K)
+    x = torch.zeros(T, K, dtype=torch.bfloat16, device="cuda")
+    x[torch.arange(T, device="cuda"), 13 * torch.arange(T, device="cuda") + 5] = 1.0
+    p = Fp32(g, T, K, N, 0, x)
+    # s from 2^-86 to 2^-84 and b = -8 s: |s q + b| is 0 or at least |s|
+    s = torch.exp2(torch.randint(-86, -84, (N, K // 64), generator=g, device="cuda").float())
+    s = s * (1 + torch.randint(0, 128, s.shape, generator=g, device="cuda") / 128.0)
+    p.params.copy_(torch.stack([s, -8 * s], dim=-1).to(torch.bfloat16))
+    lora.lora_decode_q4([p.proj()], None, 0)
+    y = torch.empty(T, N, dtype=torch.bfloat16, device="cuda")
+    st = lora.make_shape(T, K, N, 0, 1.0)
+    ws = G.workspace(lora.lora_workspace_size(st, lora.LORA_FWD))
+    lora.lora_linear_fwd_q4(st, x, lora.make_q4(p.codes, p.params), None, None, y, None, ws, ws.numel())
+    torch.cuda.synchronize()
+    assert torch.equal(p.y(), y) and float(y.abs().max()) < 2.0 ** -80
+    assert torch.equal(y.float(), x.float() @ p.weight().T)
