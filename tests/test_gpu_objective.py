@@ -404,3 +404,45 @@ def test_rows_whose_weight_rounds_to_zero(lens, reduction):
     t.dh_nll[2] = float("inf")
     policy(t, [1.0] * len(lens), False, reduction=reduction, scale=1.0)
     assert t.w[3] == 0 and (t.dh[2] == 0).all() and torch.isfinite(t.dh).all()
+
+
+@pytest.mark.parametrize("lens", [[30, 40, 50, 7], [3000, 40, 900, 7]])
+@pytest.mark.parametrize("which", ["policy", "pref"])
+def test_in_a_graph(lens, which):
+    """Captured once, replayed on other values in place."""
+    t = Tokens(70, lens, d=72)
+    adv = f32([0.5, -1.0, 2.0, 0.1])
+    extra = torch.zeros(4, device="cuda")
+    if which == "policy":
+        args = lora.make_policy_args(t.T, 4, t.d, t.doff, t.dev["nll"], t.dev["old"], adv, t.loss, ref_nll=t.dev["ref"],
+                                     mask=t.dmask, beta=0.05, reduction=MEAN_SEQS, stats=extra, **t.outputs())
+        fn, size = lora.lora_policy_fwd_bwd, lora.lora_policy_workspace_size(args)
+    else:
+        args = lora.make_pref_args(t.T, 2, t.d, t.doff, t.dev["nll"], t.loss, ref_nll=t.dev["ref"], mask=t.dmask,
+                                   rewards=extra, **t.outputs())
+        fn, size = lora.lora_pref_fwd_bwd, lora.lora_pref_workspace_size(args)
+    ws = G.workspace(size)
+    fn(args, ws, ws.numel())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fn(args, ws, ws.numel())
+    outs = [t.loss[:1], t.w[1:-1], t.dh[:t.T], extra]
+    last = None
+    for seed in (71, 72):
+        other = Tokens(seed, lens, d=72)
+        for k in ("nll", "old", "ref"):
+            t.dev[k].copy_(other.dev[k])
+        t.dmask.copy_(other.dmask)
+        t.dh_nll.copy_(other.dh_nll)
+        fn(args, ws, ws.numel())
+        torch.cuda.synchronize()
+        want = [o.clone() for o in outs]
+        for o in outs:
+            o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, outs)) and torch.isfinite(want[0]).all()
+        assert last is None or not torch.equal(last[0], want[0])
+        last = want
+    assert lora.lora_read_status() == lora.LORA_OK
