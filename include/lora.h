@@ -302,7 +302,9 @@ int lora_decode_q4(const lora_proj* projs, int n_proj, void* workspace, size_t w
 
 /* ---- Policy and preference losses ---------------------------------------
  * Both take the tokens' negative log-probabilities under the model, nll_t =
- * -log p_t (the token_loss of lora_ce_fwd_bwd), and hand back the loss, its
+ * -log p_t (the token_loss of lora_ce_fwd_bwd without a topk table; with one it
+ * is -log of the probability within that call's J, and nll, old_nll and ref_nll
+ * compare only where their calls had the same J), and hand back the loss, its
  * derivative by each of them, and the gradient of the hidden states: with the
  * rows d nll_t / d h_t that lora_ce_fwd_bwd writes into its dh,
  *     dh_t = (d loss / d nll_t) * dh_nll_t,

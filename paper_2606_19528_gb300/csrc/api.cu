@@ -2200,8 +2200,9 @@ int clip_batches(const lora_grad* grads, int n, int* partials, Launch launch) {
   return b.n || !*partials ? flush() : LORA_OK;
 }
 
-// What the sum leaves in L2 for the scaling.  97 MB that were not there before take 47.3 us with 0 (as without any
-// policy), 47.0 with 40 MB, 44.9 with 60, 44.4 with 80; the same 97 MB call after call 43.0, 40.8, 39.8 and 41.1.
+// What the sum leaves in L2 for the scaling.  97 MB that were not there before take 47.6 us with 0 (47.5 without any
+// policy), 49.4 with 20 MB, 47.0 with 40, 45.0 with 60, 44.5 with 80; the same 97 MB call after call 44.1, 43.8, 43.3,
+// 42.0 and 42.0.
 constexpr double kClipKeepBytes = 60e6;
 
 // *batches: of the launches of the call.

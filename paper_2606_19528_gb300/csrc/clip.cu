@@ -10,8 +10,8 @@
 //   clip_scale_kernel  every CTA adds these up again in the same order, then scales, from the last piece to the first:
 //                      what was read last is still in L2
 // Many tensors are bound by memory: a read for the norm, a read from L2 or HBM and a write for the scaling.  What the
-// sum reads last is asked to stay in L2, all else to leave first (28 layers of 16 tensors, 97 MB: 39.8 us call after
-// call, 44.9 where nothing was in L2 before; 194 MB at the copy rate take 28.7, 291 take 43).  Few tensors are bound by
+// sum reads last stays in L2, all else is asked to leave first (28 layers of 16 tensors, 97 MB: 42.0 us call after
+// call, 45.0 where nothing was in L2 before; 194 MB at the copy rate take 28.7, 291 take 43).  Few tensors are bound by
 // the chain launch, load, sum, exchange, store: 4.0 us for four tensors, 0.66 MB.
 // FP64 is scarce on this GPU (about 2 operations a clock and SM), so a lane's 16 squares are summed in fp32 and these
 // sums as pairs of fp32; only the warps' sums are added in fp64.  The tensors' table is a kernel argument: no copy
@@ -79,10 +79,13 @@ __device__ __forceinline__ int edge_index(const Piece& p, int lane) {
   return i < p.n ? i : -1;
 }
 
-// L2 policies: what stays for the scaling, and what is read for the last time or will not stay anyway.
+// L2 policies: what stays for the scaling, and what is read for the last time or will not stay anyway.  What stays has the
+// normal priority: lines read as evict_last held on to L2 long after the call, and the calls behind it paid for them (a
+// training layer of 256 tokens 124.1 for 122.8 us, the second of two copies of 40 MB 17.5 for 14.3), while the call
+// itself took the same time.
 __device__ __forceinline__ uint64_t policy_keep() {
   uint64_t v;
-  asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(v));
+  asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(v));
   return v;
 }
 __device__ __forceinline__ uint64_t policy_pass() {
